@@ -161,6 +161,66 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
                                      int64_t* whole, int32_t* slices);
 
 /* ------------------------------------------------------------------------
+ * Self-attention that visits the keys which matter and no others, for callers that run a block's operations themselves: queries
+ * and keys rotated by positions on any axes, their means over blocks, the choice of key blocks by the score of the means, and
+ * attention over the chosen blocks. The layouts are those of chorus_qk_norm_rope, chorus_v_transpose and chorus_attention, so each call
+ * stands in for, or behind, one of those. All are asynchronous on `stream` and allocate nothing.
+ *
+ * chorus_rope_axes: optional RMSNorm (eps 1e-6), rotation, output factor, bf16 rows -> head-major bf16.
+ *   in    dev bf16, row i at in + i*ld, H*dh values (ld >= H*dh, ld % 8 == 0; dh in {64, 128})
+ *   norm  CHORUS_ROPE_NORM_NONE; _WIDTH: over the H*dh values of a row, gain dev [H*dh] fp32; _HEAD: over each head's dh values,
+ *         gain dev [dh] fp32, the same for every head
+ *   pos   dev [L, n_axes] fp32: a token's coordinates (whole or not: stretched grids, shared text positions)
+ *   freq, axis  dev [n_pairs] fp64 and int32: pair p turns by pos[axis[p]] * freq[p] radians, formed in fp64; a pair whose axis is
+ *         outside [0, n_axes) does not turn. n_pairs <= dh / 2; the values behind the pairs pass through (normalised, not turned)
+ *   layout  CHORUS_ROPE_PAIRS: pair p is values 2p, 2p + 1 of a head; _HALVES: values p, n_pairs + p (n_pairs % 8 == 0)
+ *   out   dev bf16 [H, Lpad, dh]; rows L..Lpad-1 are written as zeros; must not overlap `in`
+ *   out_scale  as chorus_qk_norm_rope
+ * chorus_rope_axes_table: host only; the usual table for axes of dims[k] values of a head each (even, at most 128 together):
+ *   n_pairs = sum(dims) / 2 entries, axis after axis, freq = theta^(-2 i / dims[k]) for i = 0 .. dims[k] / 2 - 1.
+ *
+ * chorus_block_mean: out dev bf16 [H, nB, dh] = the mean of each `block` consecutive rows of X dev bf16 [H, Lpad, dh], nB =
+ *   ceil(L / block); a short last block is the mean of its own rows. block: CHORUS_BLOCK_QUERIES or CHORUS_BLOCK_KEYS.
+ *
+ * chorus_block_select: for each of H heads and nq rows of Qm the `keep` of nk rows of Km that come first by class, score, index:
+ *   Qm dev bf16 [H, nq, dh], Km dev bf16 [Hk, nk, dh] (H % Hk == 0; head h reads h / (H / Hk)); score = Qm . Km, exact products added in
+ *   fp64, NaN below every number, the higher first, equal ones by ascending index
+ *   rule   dev uint8 [nk] or NULL: 1 = ahead of all others, 2 = never, anything else by its score
+ *   blocks dev int32 [H, nq, keep]: ascending, -1 behind the last
+ *   nk from 1 to CHORUS_BLOCK_SELECT_MAX (CHORUS_E_SHAPE), keep >= 1.
+ *
+ * chorus_attention_blocks: O = softmax(Q K^T / sqrt(dh)) V with the queries of block a (CHORUS_BLOCK_QUERIES of them) of head h seeing
+ *   the keys of the key blocks (CHORUS_BLOCK_KEYS keys) in blocks[h, a, :] only. An entry outside [0, ceil(Lk / 64)) is passed over, so
+ *   -1 fills a shorter list; the order does not matter but to the rounding; a block that is listed twice counts twice. A row that sees
+ *   no key, or only logits of -inf, is zeros. Keys and values that no list names are not read.
+ *   Q dev bf16 [H, LqPad, dh], K dev bf16 [Hk, LkPad, dh], Vt dev bf16 [Hk*dh, LkPad] in chorus_v_transpose's layout
+ *   (H % Hk == 0; head h reads h / (H / Hk)), O dev bf16 [Lq, H*dh], blocks dev int32 [H, ceil(Lq / 128), keep]
+ *   prescaled  non-zero: Q holds the queries multiplied by CHORUS_ATTENTION_Q_PRESCALE(dh), as for chorus_attention's variant 6
+ *   ws    dev, chorus_attention_blocks_workspace_bytes bytes (0: none, ws may be NULL)
+ *   dh in {64,128}; LkPad % 64 == 0, LkPad >= Lk >= 1; rows and columns beyond Lq and Lk are padding (finite values).
+ * Errors: CHORUS_E_ARG, CHORUS_E_SHAPE, CHORUS_E_WORKSPACE, CHORUS_E_HIP.
+ * ------------------------------------------------------------------------ */
+#define CHORUS_ROPE_NORM_NONE 0
+#define CHORUS_ROPE_NORM_WIDTH 1
+#define CHORUS_ROPE_NORM_HEAD 2
+#define CHORUS_ROPE_PAIRS 0
+#define CHORUS_ROPE_HALVES 1
+int32_t chorus_rope_axes_table(int32_t n_axes, const int32_t* dims, double theta, double* freq, int32_t* axis, int32_t* n_pairs);
+int32_t chorus_rope_axes(const uint16_t* in, int64_t ld, const float* gain, int32_t norm, uint16_t* out, int64_t L, int64_t Lpad,
+                         int32_t H, int32_t dh, const float* pos, int32_t n_axes, const double* freq, const int32_t* axis,
+                         int32_t n_pairs, int32_t layout, float out_scale, void* stream);
+#define CHORUS_BLOCK_QUERIES 128
+#define CHORUS_BLOCK_KEYS 64
+#define CHORUS_BLOCK_SELECT_MAX 16384
+int32_t chorus_block_mean(const uint16_t* X, uint16_t* out, int64_t L, int64_t Lpad, int32_t H, int32_t dh, int32_t block, void* stream);
+int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_t* rule, int32_t* blocks, int64_t nq, int64_t nk, int32_t H,
+                            int32_t Hk, int32_t dh, int32_t keep, void* stream);
+size_t chorus_attention_blocks_workspace_bytes(int64_t Lq, int32_t H, int32_t dh, int32_t keep);
+int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint16_t* Vt, uint16_t* O, const int32_t* blocks, int32_t keep,
+                                int64_t Lq, int64_t Lk, int64_t LqPad, int64_t LkPad, int32_t H, int32_t Hk, int32_t dh, int32_t prescaled,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Step glue (stand-ins that close the denoising loop around the blocks; the
  * paper's sampler is DPM++ with default settings, whose coefficients it does not
  * give, so an Euler update x <- x + dsigma * v is used).

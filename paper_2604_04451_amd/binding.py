@@ -168,6 +168,12 @@ def _bind_ops(lib):
         "chorus_attention_slices_plan": (i32, [i64, i32, i32, i32, sz, sz, C.POINTER(i64), C.POINTER(i32)]),
         "chorus_gemm_bf16_chain": (i32, [vp, vp, i64, i32, i32, vp, vp, vp, vp, f32, i32, i32, vp, i32, vp]),
         "chorus_gemm_bf16_chain_plan": (i32, [i64, i32, i32, sz, sz, C.POINTER(GemmPlan), C.POINTER(i32)]),
+        "chorus_rope_axes_table": (i32, [i32, C.POINTER(i32), C.c_double, C.POINTER(C.c_double), C.POINTER(i32), C.POINTER(i32)]),
+        "chorus_rope_axes": (i32, [vp, i64, vp, i32, vp, i64, i64, i32, i32, vp, i32, vp, vp, i32, i32, f32, vp]),
+        "chorus_block_mean": (i32, [vp, vp, i64, i64, i32, i32, i32, vp]),
+        "chorus_block_select": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, vp]),
+        "chorus_attention_blocks_workspace_bytes": (sz, [i64, i32, i32, i32]),
+        "chorus_attention_blocks": (i32, [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, i32, vp, sz, vp]),
         "chorus_glue_workspace_bytes": (sz, [i32, i32, i64]),
         "chorus_patch_embed": (i32, [vp, i32, i32, i32, i32, i32, i32, vp, i64, GW, i32, vp, vp, sz, vp]),
         "chorus_head_update": (i32, [vp, vp, i64, vp, GW, vp, f32, i32, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
@@ -709,6 +715,94 @@ def chorus_attention_slices_plan(L, H, dh, cus, first_bytes, rest_bytes):
     _status("chorus_attention_slices_plan", load().chorus_attention_slices_plan(L, H, dh, cus, first_bytes, rest_bytes,
                                                                                 C.byref(whole), C.byref(slices)))
     return whole.value, slices.value
+
+
+# ------------------------------------------- attention over selected blocks of keys
+
+ROPE_NORM_NONE, ROPE_NORM_WIDTH, ROPE_NORM_HEAD = 0, 1, 2
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+BLOCK_QUERIES, BLOCK_KEYS, BLOCK_SELECT_MAX = 128, 64, 16384
+
+
+def chorus_rope_axes_table(dims, theta=10000.0, device="cuda"):
+    """The usual frequencies for axes of dims[k] values of a head each: (freq float64 [n], axis int32 [n]) on `device`."""
+    dims = [int(d) for d in dims]
+    freq, axis, n = (C.c_double * 64)(), (C.c_int32 * 64)(), C.c_int32(0)
+    _status("chorus_rope_axes_table", load().chorus_rope_axes_table(len(dims), (C.c_int32 * len(dims))(*dims), float(theta), freq, axis,
+                                                                    C.byref(n)))
+    return (torch.tensor(freq[:n.value], dtype=torch.float64, device=device),
+            torch.tensor(axis[:n.value], dtype=torch.int32, device=device))
+
+
+def chorus_rope_axes(inp, col0, gain, norm, out, L, H, dh, pos, freq, axis, layout=ROPE_PAIRS, out_scale=1.0):
+    """inp: bf16 [L, ld]; the H*dh columns starting at col0 are normalised, rotated by pos [L, n_axes] and written head-major."""
+    lib = load()
+    _chk(inp, torch.bfloat16, "inp")
+    _chk(out, torch.bfloat16, "out")
+    _chk(gain, torch.float32, "gain", (H * dh if norm == ROPE_NORM_WIDTH else dh,))
+    _chk(pos, torch.float32, "pos")
+    _chk(freq, torch.float64, "freq")
+    _chk(axis, torch.int32, "axis", freq.shape)
+    ld, Lpad = inp.shape[1], out.shape[1]
+    if tuple(out.shape) != (H, Lpad, dh) or col0 < 0 or col0 + H * dh > ld or inp.shape[0] < L or pos.dim() != 2 or pos.shape[0] < L:
+        raise TypeError("shape mismatch")
+    _status("chorus_rope_axes", lib.chorus_rope_axes(inp.data_ptr() + 2 * col0, ld, _p(gain), int(norm), _p(out), L, Lpad, H, dh, _p(pos),
+                                                     pos.shape[1], _p(freq), _p(axis), freq.numel(), int(layout), float(out_scale),
+                                                     _stream()))
+    return out
+
+
+def chorus_block_mean(X, out, L, block):
+    """out bf16 [H, ceil(L / block), dh]: means over blocks of rows of X [H, Lpad, dh]; block BLOCK_QUERIES or BLOCK_KEYS."""
+    lib = load()
+    _chk(X, torch.bfloat16, "X")
+    H, Lpad, dh = X.shape
+    _chk(out, torch.bfloat16, "out", (H, -(-L // block), dh))
+    _status("chorus_block_mean", lib.chorus_block_mean(_p(X), _p(out), L, Lpad, H, dh, int(block), _stream()))
+    return out
+
+
+def chorus_block_select(Qm, Km, blocks, rule=None):
+    """blocks int32 [H, nq, keep]: for each row of Qm [H, nq, dh] the key blocks kept by its score with Km [Hk, nk, dh]."""
+    lib = load()
+    _chk(Qm, torch.bfloat16, "Qm")
+    _chk(Km, torch.bfloat16, "Km")
+    H, nq, dh = Qm.shape
+    Hk, nk, _ = Km.shape
+    _chk(rule, torch.uint8, "rule", (nk,))
+    _chk(blocks, torch.int32, "blocks")
+    if Km.shape[2] != dh or blocks.dim() != 3 or tuple(blocks.shape[:2]) != (H, nq):
+        raise TypeError("shape mismatch")
+    _status("chorus_block_select", lib.chorus_block_select(_p(Qm), _p(Km), _p(rule), _p(blocks), nq, nk, H, Hk, dh, blocks.shape[2],
+                                                           _stream()))
+    return blocks
+
+
+def chorus_attention_blocks_workspace_bytes(Lq, H, dh, keep) -> int:
+    return load().chorus_attention_blocks_workspace_bytes(Lq, H, dh, keep)
+
+
+def chorus_attention_blocks(Q, K, Vt, O, blocks, Lq, Lk, prescaled=False, ws=None):
+    """Attention of the queries of a block to the key blocks in its row of blocks int32 [H, ceil(Lq / 128), keep]."""
+    lib = load()
+    for n, t in (("Q", Q), ("K", K), ("Vt", Vt), ("O", O)):
+        _chk(t, torch.bfloat16, n)
+    _chk(blocks, torch.int32, "blocks")
+    H, LqPad, dh = Q.shape
+    Hk, LkPad, _ = K.shape
+    if K.shape[2] != dh or tuple(Vt.shape) != (Hk * dh, LkPad) or O.shape[1] != H * dh or O.shape[0] < Lq:
+        raise TypeError("shape mismatch")
+    if blocks.dim() != 3 or tuple(blocks.shape[:2]) != (H, -(-Lq // BLOCK_QUERIES)):
+        raise TypeError("blocks: wrong shape")
+    keep = blocks.shape[2]
+    _chk(ws, torch.uint8, "ws")
+    if ws is None:
+        need = lib.chorus_attention_blocks_workspace_bytes(Lq, H, dh, keep)
+        ws = _ws(need, Q.device) if need else None
+    _status("chorus_attention_blocks", lib.chorus_attention_blocks(_p(Q), _p(K), _p(Vt), _p(O), _p(blocks), keep, Lq, Lk, LqPad, LkPad, H,
+                                                                   Hk, dh, int(prescaled), _p(ws), 0 if ws is None else ws.numel(),
+                                                                   _stream()))
+    return O
 
 
 # ------------------------------------------------------------- step glue
