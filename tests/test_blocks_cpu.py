@@ -67,10 +67,27 @@ def _attend(lib, Q=P16, K=P16, Vt=P16, O=P16, blocks=P16, keep=4, Lq=100, Lk=200
     (dict(Hk=0), B.E_ARG), (dict(keep=0), B.E_ARG), (dict(Q=NULL), B.E_ARG), (dict(K=NULL), B.E_ARG), (dict(Vt=NULL), B.E_ARG),
     (dict(O=NULL), B.E_ARG), (dict(blocks=NULL), B.E_ARG), (dict(Q=P8), B.E_ARG), (dict(Vt=P8), B.E_ARG), (dict(blocks=P8), B.E_ARG),
     (dict(ws=P8), B.E_ARG), (dict(Lk=0), B.E_SHAPE), (dict(LkPad=224), B.E_SHAPE), (dict(dh=96), B.E_SHAPE), (dict(Hk=3), B.E_SHAPE),
-    (dict(LkPad=1 << 32, Lk=1 << 32), B.E_SHAPE), (dict(Lq=1 << 40, LqPad=1 << 40), B.E_SHAPE), (dict(Lq=0), B.OK),
+    (dict(LkPad=1 << 32, Lk=1 << 32), B.E_SHAPE), (dict(LkPad=(1 << 22) + 64), B.E_SHAPE), (dict(Lq=1 << 40, LqPad=1 << 40), B.E_SHAPE),
+    (dict(Lq=(1 << 31) - 1, LqPad=1 << 31, H=400, Hk=400), B.E_SHAPE), (dict(Lq=0), B.OK),
+    # few lists of many blocks are cut into slices, which need a workspace
+    (dict(Lq=1, keep=1000), B.E_WORKSPACE), (dict(Lq=1, keep=1000, ws=P16, ws_bytes=1 << 16), B.E_WORKSPACE),
 ])
 def test_attention_blocks_refuses(change, want):
     assert _attend(P.load(), **change) == want
+
+
+def test_attention_blocks_workspace():
+    """Slices only where lists leave compute units idle, 64 of them at most, 128 rows of fp32 results and 8 bytes each."""
+    need = P.load().chorus_attention_blocks_workspace_bytes
+    row = lambda dh: 128 * (4 * dh + 8)  # noqa: E731
+    assert need(32768, 2, 128, 100) == need(16384, 4, 64, 1000) == 0            # 512 lists: a full round
+    for Lq, H, dh, keep in ((1, 1, 128, 5000), (60, 12, 128, 256), (128, 40, 64, 600), (5000, 16, 128, 900)):
+        lists = -(-Lq // 128) * H % 512
+        n, over = divmod(need(Lq, H, dh, keep), lists * row(dh))
+        assert not over and 2 <= n <= min(64, keep), (Lq, H, dh, keep, n)
+    assert need(1, 1, 128, 1) == need(128, 4, 64, 3) == 0                       # nothing to cut
+    assert need(0, 4, 64, 100) == need(-1, 4, 64, 100) == need(1, 0, 64, 100) == need(1, 4, 96, 100) == need(1, 4, 64, 0) == 0
+    assert need(1 << 40, 4, 64, 100) == need((1 << 31) - 1, 1 << 20, 64, 100) == 0
 
 
 def test_rope_axes_table():
