@@ -51,20 +51,21 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
 // How far a score can be off: products of bf16 are exact in fp32, and whatever the order of a sum of DH <= 128 of them, each of its
 // additions is off by at most 2^-23 of the sum of magnitudes, itself at most |q| |k|: kBound |q| max |k|, and a trace for values
 // that are flushed. Norms come from the same pipe (the diagonal of K K^T) and are within 2^-16 of their values, which kBound has room for.
+// Where that bound is finite so is every score; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
 //
-// A score is held as 32 bits whose unsigned order is the order of the floats; 0 stands for "out" and kIn for "in", which no finite
-// float has. Under `always` a block is in from the start, under `never` out.
+// Bound by the vector pipe: a row of 1182 blocks costs about 500 instructions of its wave, 20 of them for each look at all its scores. The fast
+// path therefore stays in floats: a block that is in whatever its score (`always`) scores +inf, one that is out -inf.
 // ---------------------------------------------------------------------------
-constexpr uint32_t kIn = 0xffffffffu, kOut = 0u;
+constexpr uint32_t kIn = 0xffffffffu, kOut = 0u;  // the same two as codes: no finite float has them
 constexpr float kBound = 1.05f / 65536.0f;
-constexpr int kSelectThreads = 512;
 
+// Codes: 32 bits whose unsigned order is the order of the floats, both zeros alike.
 __device__ __forceinline__ uint32_t ordered(float f) {
   const uint32_t b = __float_as_uint(f + 0.0f);
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t v) { return __uint_as_float(v >> 31 ? v & 0x7fffffffu : ~v); }
-// NaN below every number, both zeros alike
+// NaN below every number
 __device__ __forceinline__ uint64_t ordered(double s) {
   if (s != s) return 0;
   const uint64_t b = __builtin_bit_cast(uint64_t, s + 0.0);
@@ -83,62 +84,183 @@ __device__ __forceinline__ uint32_t wave_extreme(uint32_t v) {
   v = of(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, false));
   return __builtin_amdgcn_readfirstlane(of(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, false)));
 }
+__device__ __forceinline__ int lanes_below(uint64_t mask, int more) {  // of the mask's lanes, and `more`
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, more));
+}
 
 // The score of a row of queries and a block of keys in fp64: exact, unless terms are 2^30 apart.
 template <int DH>
 __device__ __forceinline__ uint64_t exact_score(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k) {
-  double s = 0.0;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 4
   for (int d = 0; d < DH; d += 8) {
     const u32x4 a = *reinterpret_cast<const u32x4*>(q + d), b = *reinterpret_cast<const u32x4*>(k + d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      s = __builtin_fma((double)__uint_as_float(a[e] << 16), (double)__uint_as_float(b[e] << 16), s);
-      s = __builtin_fma((double)__uint_as_float(a[e] & 0xffff0000u), (double)__uint_as_float(b[e] & 0xffff0000u), s);
+      s[e] = __builtin_fma((double)__uint_as_float(a[e] << 16), (double)__uint_as_float(b[e] << 16), s[e]);
+      s[e] = __builtin_fma((double)__uint_as_float(a[e] & 0xffff0000u), (double)__uint_as_float(b[e] & 0xffff0000u), s[e]);
     }
   }
-  return ordered(s);
+  return ordered((s[0] + s[1]) + (s[2] + s[3]));
 }
 
-// The row's scores, one in 64 a lane: in registers (NV of them), or in LDS where there are more.
+// A row's scores, one in 64 a lane: in registers (NV of them), or in LDS where there are more.
 template <int NV>
 struct Scores {
-  uint32_t reg[NV > 0 ? NV : 1];
+  float reg[NV > 0 ? NV : 1];
   uint32_t* at;  // the row in LDS, this lane's first
   int n;         // scores a lane
   __device__ __forceinline__ int count() const { return NV > 0 ? NV : n; }
-  __device__ __forceinline__ uint32_t get(int i) const { return NV > 0 ? reg[NV > 0 ? i : 0] : at[64 * i]; }
-  __device__ __forceinline__ void set(int i, uint32_t v) {
+  __device__ __forceinline__ float get(int i) const { return NV > 0 ? reg[NV > 0 ? i : 0] : __uint_as_float(at[64 * i]); }
+  __device__ __forceinline__ void set(int i, float v) {
     if (NV > 0) reg[NV > 0 ? i : 0] = v;
-    else at[64 * i] = v;
+    else at[64 * i] = __float_as_uint(v);
   }
-  template <class OF>
-  __device__ __forceinline__ int how_many(OF of) const {  // of the wave's scores
+  __device__ __forceinline__ int reach(float t) const {  // how many of the wave's scores reach t
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < count(); ++i) c += __builtin_popcountll(__ballot(of(get(i))));
+    for (int i = 0; i < count(); ++i) c += __builtin_popcountll(__ballot(get(i) >= t));
     return c;
   }
-  // The largest t that at least W scores reach, or one that exactly W reach. Bisection between the least and the largest score, of values
-  // where they are floats (a row's scores are spread like a bell, so halves of its range leave their order of magnitude in a few
-  // steps, as halves of the order of the bits do not), of the order otherwise; the latter always ends.
-  __device__ __forceinline__ uint32_t find(int W, bool floats, int& reached) const {
-    uint32_t least = kIn, most = kOut;
-#pragma unroll
-    for (int i = 0; i < count(); ++i) {
-      const uint32_t v = get(i);
-      if (v != kOut && v < least) least = v;
-      if (v != kIn && v > most) most = v;
-    }
-    uint32_t lo = wave_extreme<false>(least), hi = wave_extreme<true>(most) + 1;
-    reached = how_many([&](uint32_t v) { return v >= lo; });
-    for (int step = 0; reached != W && hi - lo > 1; ++step) {
-      uint32_t mid = lo + (hi - lo) / 2;
-      if (floats && step < 16) {
-        const uint32_t m = ordered(0.5f * unordered(lo) + 0.5f * unordered(hi));
-        if (m > lo && m < hi) mid = m;
+  // The border of the W largest, `in` of them +inf and `all` not -inf: the least of them, the next one behind, and how many reach the former (more than
+  // W where several are equal). Bisection between -bound and bound, beyond which there are finite scores on neither side: first at twice the
+  // usual size of a score and at 0, then of the values for a while (a row's scores are spread like a bell, and halves of their range
+  // come near in a few steps, as halves of the order of their bits do not), then of the order, which always ends. As soon as the border lies
+  // among 64 scores or fewer they move to a lane each, and a step costs one comparison.
+  struct Border {
+    float least, next;
+    int reached;
+  };
+  __device__ __forceinline__ Border border(int W, int in, int all, float bound, float usual, uint32_t* __restrict__ list, int lane) const {
+    uint32_t lo = __builtin_amdgcn_readfirstlane(ordered(-bound)), hi = __builtin_amdgcn_readfirstlane(ordered(bound)) + 1;
+    auto middle = [&](int step) {
+      const float half = step == 0 ? 2.0f * usual : step == 1 ? 0.f : 0.5f * unordered(lo) + 0.5f * unordered(hi);
+      const uint32_t m = __builtin_amdgcn_readfirstlane(ordered(half));
+      return step < 18 && m > lo && m < hi ? m : lo + (hi - lo) / 2;
+    };
+    int reach_lo = all, reach_hi = in, step = 0;
+    for (; reach_lo != W && hi - lo > 1 && reach_lo - reach_hi > 64; ++step) {
+      const uint32_t mid = middle(step);
+      const int c = reach(unordered(mid));
+      if (c >= W) {
+        lo = mid;
+        reach_lo = c;
+      } else {
+        hi = mid;
+        reach_hi = c;
       }
-      const int c = how_many([&](uint32_t v) { return v >= mid; });
+    }
+    const float from = unordered(lo), to = unordered(hi);
+    float least = INFINITY, next = -INFINITY;
+    if (reach_lo == W || hi - lo <= 1) {
+#pragma unroll
+      for (int i = 0; i < count(); ++i) {
+        const float x = get(i);
+        least = fminf(least, x >= from ? x : INFINITY);
+        next = fmaxf(next, x >= from ? -INFINITY : x);
+      }
+    } else {
+      int at = 0;
+#pragma unroll
+      for (int i = 0; i < count(); ++i) {
+        const float x = get(i);
+        const bool of = x >= from && x < to;
+        const uint64_t taken = __ballot(of);
+        if (of) list[lanes_below(taken, at)] = __float_as_uint(x);
+        at += __builtin_popcountll(taken);
+      }
+      __builtin_amdgcn_wave_barrier();
+      const float x = lane < at ? __uint_as_float(list[lane]) : -INFINITY;
+      const uint32_t code = ordered(x);
+      for (; reach_lo != W && hi - lo > 1; ++step) {
+        const uint32_t mid = middle(step);
+        const int c = reach_hi + __builtin_popcountll(__ballot(code >= mid && code < hi));
+        if (c >= W) {
+          lo = mid;
+          reach_lo = c;
+        } else {
+          hi = mid;
+          reach_hi = c;
+        }
+      }
+      least = code >= lo ? x : INFINITY;
+      next = code < lo ? x : -INFINITY;
+      __builtin_amdgcn_wave_barrier();
+    }
+    return Border{unordered(wave_extreme<false>(ordered(least))), unordered(wave_extreme<true>(ordered(next))), reach_lo};
+  }
+};
+
+// Writes a row's choice, the blocks whose `take` holds: ascending, then -1.
+template <class TAKE>
+__device__ __forceinline__ void put_row(int n, TAKE take, int* __restrict__ to, int keep, int lane) {
+  int put = 0;
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const bool t = take(i);
+    const uint64_t taken = __ballot(t);
+    if (t) to[lanes_below(taken, put)] = lane + 64 * i;
+    put += __builtin_popcountll(taken);
+  }
+  for (int i = put + lane; i < keep; i += 64) to[i] = -1;
+}
+
+// The choice of W where fp32 scores do not make it. It is rare, works in LDS and stays out of the row loop's registers. The row there holds
+// scores (+inf: in, -inf: out); `odd`: they say nothing, else the border is at `last`, within `off` of exact.
+template <int DH>
+__device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float last, float off, uint32_t* __restrict__ list,
+                                             const uint16_t* __restrict__ q, const uint16_t* __restrict__ km, int* __restrict__ to, int keep, int lane) {
+  // codes: kIn, kOut, or 1 for what the exact scores decide, the first 64 of which are listed
+  int open = 0, in = 0;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const uint32_t bits = at[64 * i];
+    const float f = __uint_as_float(bits);
+    const bool is_in = bits == 0x7f800000u || (!odd && f > last + 2.0f * off), is_out = bits == 0xff800000u || (!odd && f < last - 2.0f * off);
+    const uint64_t undecided = __ballot(!is_in && !is_out);
+    const int place = lanes_below(undecided, open);
+    at[64 * i] = is_in ? kIn : is_out ? kOut : 1u;
+    if (!is_in && !is_out && place < 64) list[place] = lane + 64 * i;
+    in += __builtin_popcountll(__ballot(is_in));
+    open += __builtin_popcountll(undecided);
+  }
+  __builtin_amdgcn_wave_barrier();
+  // a wave that has as many lanes: each makes an exact score and counts those that come before it
+  if (open <= 64) {
+    const int b = lane < open ? list[lane] : 0;
+    const uint64_t e = lane < open ? exact_score<DH>(q, km + (long)b * DH) : 0;
+    int before = in;
+    for (int j = 0; j < open; ++j) {  // in ascending order of index: equal scores go to the lower lane
+      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(e >> 32), j), lo = __builtin_amdgcn_readlane((uint32_t)e, j);
+      const uint64_t other = (uint64_t)hi << 32 | lo;
+      before += other > e || (other == e && j < lane);
+    }
+    if (lane < open && before < W) at[b - lane] = kIn;  // `at` is this lane's first
+    __builtin_amdgcn_wave_barrier();
+    put_row(n, [&](int i) { return at[64 * i] == kIn; }, to, keep, lane);
+    return;
+  }
+  // the 64 bits of the scores in three parts, each among those that are alike in the part before; what is alike in all goes by index
+  uint32_t from = 1, tied = kOut;
+  int equal = 0;
+  auto reach = [&](uint32_t t) {
+    int c = 0;
+    for (int i = 0; i < n; ++i) c += __builtin_popcountll(__ballot(at[64 * i] >= t));
+    return c;
+  };
+  for (int part = 0; part < 3; ++part) {
+    for (int i = 0; i < n; ++i) {
+      const uint32_t x = at[64 * i];
+      if (x != kOut && x != kIn) {
+        const uint64_t e = exact_score<DH>(q, km + (long)(lane + 64 * i) * DH);
+        at[64 * i] = 1u + (part == 0 ? (uint32_t)(e >> 33) : part == 1 ? (uint32_t)(e >> 2) & 0x7fffffffu : (uint32_t)e & 3u);
+      }
+    }
+    uint32_t lo = 1, hi = kIn;  // all that are open reach the one, fewer than W the other
+    int reached = reach(lo);
+    while (reached != W && hi - lo > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      const int c = reach(mid);
       if (c >= W) {
         lo = mid;
         reached = c;
@@ -146,192 +268,179 @@ struct Scores {
         hi = mid;
       }
     }
-    return lo;
-  }
-};
-
-// Writes the row's choice: what reaches `from`, and the first `equal` of those that are `tied`, which is below it; ascending, then -1.
-template <int NV>
-__device__ __forceinline__ void put_row(const Scores<NV>& v, uint32_t from, uint32_t tied, int equal, int* __restrict__ to, int keep,
-                                        int lane) {
-  int put = 0;
-  const uint64_t below = (1ull << lane) - 1;
-#pragma unroll
-  for (int i = 0; i < v.count(); ++i) {
-    const uint32_t x = v.get(i);
-    const uint64_t ties = __ballot(x == tied && x < from);
-    const bool take = x >= from || (x == tied && __builtin_popcountll(ties & below) < equal);
-    const uint64_t taken = __ballot(take);
-    if (take) to[put + __builtin_popcountll(taken & below)] = lane + 64 * i;
-    put += __builtin_popcountll(taken);
-    equal -= __builtin_popcountll(ties);
-  }
-  for (int i = put + lane; i < keep; i += 64) to[i] = -1;
-}
-
-// The choice of W by exact scores among those that are neither in nor out. Their 64 bits are compared in three parts, each among those that
-// are alike in the part before; what is alike in all goes by index. In LDS, as this is rare and its loops are long.
-template <int DH>
-__device__ __noinline__ void put_row_exactly(Scores<0> v, int W, const uint16_t* __restrict__ q, const uint16_t* __restrict__ km,
-                                             int* __restrict__ to, int keep, int lane) {
-  uint32_t from = 1, tied = kIn;
-  int equal = 0;
-  for (int part = 0; part < 3; ++part) {
-    for (int i = 0; i < v.n; ++i) {
-      const uint32_t x = v.get(i);
-      if (x != kOut && x != kIn) {
-        const uint64_t e = exact_score<DH>(q, km + (long)(lane + 64 * i) * DH);
-        v.set(i, 1u + (part == 0 ? (uint32_t)(e >> 33) : part == 1 ? (uint32_t)(e >> 2) & 0x7fffffffu : (uint32_t)e & 3u));
-      }
-    }
-    int reached;
-    from = v.find(W, false, reached);
+    from = lo;
+    tied = kOut;
     if (reached == W) break;
-    tied = from;
+    tied = lo;
     from = kIn;
-    equal = W - v.how_many([&](uint32_t x) { return x > tied; });
-    for (int i = 0; i < v.n; ++i) {
-      const uint32_t x = v.get(i);
-      if (x != kOut && x != kIn && x != tied) v.set(i, x > tied ? kIn : kOut);
+    equal = W - reach(lo + 1);
+    for (int i = 0; i < n; ++i) {
+      const uint32_t x = at[64 * i];
+      if (x != kOut && x != kIn && x != tied) at[64 * i] = x > tied ? kIn : kOut;
     }
   }
-  put_row(v, from, tied, from == kIn ? equal : 0, to, keep, lane);
+  put_row(n, [&](int i) {
+    const uint32_t x = at[64 * i];
+    const uint64_t ties = __ballot(tied != kOut && x == tied);
+    const bool take = x >= from || (tied != kOut && x == tied && lanes_below(ties, 0) < equal);
+    equal -= __builtin_popcountll(ties);
+    return take;
+  }, to, keep, lane);
 }
 
-template <int DH, int NV>
-__global__ __launch_bounds__(kSelectThreads) void block_select_kernel(const uint16_t* __restrict__ Qm, const uint16_t* __restrict__ Km,
-                                                                      const uint8_t* __restrict__ rule, int* __restrict__ blocks, int nq,
-                                                                      int nk, int group, int keep, int R, int stride, int tiles) {
-  constexpr int KC = DH / 32, WAVES = kSelectThreads / 64;
-  extern __shared__ __attribute__((aligned(16))) uint8_t s_raw[];
-  float* score = reinterpret_cast<float*>(s_raw);  // [R][stride]
-  __shared__ uint32_t s_k2;                        // the largest squared norm of a block of keys
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// T: 16-row tiles of queries, R = 16 T rows or fewer where T is 1. THREADS: 1024 where a lane's scores fit the registers of four waves a SIMD.
+template <int DH, int NV, int T, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select_kernel(const uint16_t* __restrict__ Qm, const uint16_t* __restrict__ Km,
+                                                                                        const uint8_t* __restrict__ rule, int* __restrict__ blocks, int nq,
+                                                                                        int nk, int group, int keep, int R, int stride, int tiles) {
+  constexpr int KC = DH / 32, WAVES = THREADS / 64;
+  extern __shared__ __attribute__((aligned(16))) uint32_t score[];  // [R][stride]
+  __shared__ uint32_t s_k2[WAVES];        // the largest squared norm of a block of keys that a wave met
+  __shared__ float s_q2[16 * T];          // the rows' squared norms
+  __shared__ uint32_t s_list[WAVES][64];  // scores at a border, and blocks that the fp32 scores leave open
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int at = xcd_remap(blockIdx.x, gridDim.x), head = at / tiles, first = (at - head * tiles) * R;
   const uint16_t* q0 = Qm + (long)head * nq * DH;
   const uint16_t* km = Km + (long)(head / group) * nk * DH;
-  if (threadIdx.x == 0) s_k2 = 0;
-  __syncthreads();
+  const int strips = (nk + 15) / 16, last = strips - 1;
+  // the rules of this lane's blocks, on their way while the scores are made
+  uint32_t of_block[NV > 0 ? NV : 1];
+  auto rule_of = [&](int i) { return lane + 64 * i >= nk ? 2u : rule ? (uint32_t)rule[lane + 64 * i] : 0u; };
+#pragma unroll
+  for (int i = 0; i < (NV > 0 ? NV : 1); ++i) of_block[i] = rule_of(i);
   {
     const int l16 = lane & 15, g = lane >> 4;
-    bf16x8 qf[KC];
-    const int row = first + l16 < nq ? first + l16 : nq - 1;
+    bf16x8 qf[T][KC];
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) qf[kc] = *reinterpret_cast<const bf16x8*>(q0 + (long)row * DH + 32 * kc + 8 * g);
-    float k2 = 0.f;
-    for (int strip = wave; strip * 16 < nk; strip += WAVES) {
-      const int key = strip * 16 + l16 < nk ? strip * 16 + l16 : nk - 1;
-      bf16x8 kf[KC];
+    for (int t = 0; t < T; ++t) {
+      const int row = first + 16 * t + l16 < nq ? first + 16 * t + l16 : nq - 1;
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) kf[kc] = *reinterpret_cast<const bf16x8*>(km + (long)key * DH + 32 * kc + 8 * g);
-      f32x4 s = {0.f, 0.f, 0.f, 0.f}, n2 = {0.f, 0.f, 0.f, 0.f};
+      for (int kc = 0; kc < KC; ++kc) qf[t][kc] = *reinterpret_cast<const bf16x8*>(q0 + (long)row * DH + 32 * kc + 8 * g);
+    }
+    // strips of 16 keys, two in flight behind the one in use; behind the last strip the last again
+    const uint32_t whole = l16 * DH + 8 * g, cut = (16 * last + l16 < nk ? l16 : nk - 1 - 16 * last) * DH + 8 * g;
+    bf16x8 kf[3][KC];
+    auto fetch = [&](bf16x8(&to)[KC], int strip) {
+      strip = strip < last ? strip : last;
+      const uint16_t* from = km + (long)strip * 16 * DH;
+      const uint32_t off = strip == last ? cut : whole;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) to[kc] = *reinterpret_cast<const bf16x8*>(from + off + 32 * kc);
+    };
+    uint32_t k2 = 0;  // as bits: a NaN is above all numbers, and the sign of one is dropped
+    uint32_t* to = score + (long)l16 * stride + 4 * g;
+    auto use = [&](const bf16x8(&kf)[KC], int strip) {
+      f32x4 s[T], n2 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < T; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) {
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kc], qf[kc], s, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < T; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kc], qf[t][kc], s[t], 0, 0, 0);
         n2 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kc], kf[kc], n2, 0, 0, 0);
       }
+      // the diagonal is with the lanes g = l16 / 4, in element l16 % 4
+      const float d = l16 & 2 ? (l16 & 1 ? n2[3] : n2[2]) : (l16 & 1 ? n2[1] : n2[0]);
+      const uint32_t bits = __float_as_uint(d) & 0x7fffffffu;
+      k2 = bits > k2 ? bits : k2;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (4 * g + i == l16) k2 = n2[i] >= k2 || n2[i] != n2[i] ? n2[i] : k2;  // a NaN stays
-      if (l16 < R) *reinterpret_cast<f32x4*>(score + (long)l16 * stride + strip * 16 + 4 * g) = s;
+      for (int t = 0; t < T; ++t)
+        if (T > 1 || l16 < R) *reinterpret_cast<u32x4*>(to + (long)t * 16 * stride + strip * 16) = __builtin_bit_cast(u32x4, s[t]);
+    };
+    fetch(kf[0], wave);
+    fetch(kf[1], wave + WAVES);
+    // behind the last strip, what a wave reads of a row is zeros
+    const int pad = (64 - strips * 16 % 64) % 64;
+    for (int row = wave; row < R; row += WAVES)
+      if (lane < pad) score[(long)row * stride + strips * 16 + lane] = 0;
+    for (int strip = wave; strip <= last; strip += 3 * WAVES) {
+      fetch(kf[2], strip + 2 * WAVES);
+      use(kf[0], strip);
+      if (strip + WAVES > last) break;
+      fetch(kf[0], strip + 3 * WAVES);
+      use(kf[1], strip + WAVES);
+      if (strip + 2 * WAVES > last) break;
+      fetch(kf[1], strip + 4 * WAVES);
+      use(kf[2], strip + 2 * WAVES);
     }
-    if (k2 != k2) k2 = INFINITY;
-    atomicMax(&s_k2, __float_as_uint(k2));
+    k2 = wave_extreme<true>(g == l16 >> 2 ? k2 : 0);
+    if (lane == 0) s_k2[wave] = k2;
+    if (wave == 0) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        float q2 = 0.f;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) q2 = __builtin_fmaf((float)qf[t][kc][e], (float)qf[t][kc][e], q2);
+        q2 += swap_rows16(q2);
+        q2 += swap_halves(q2);
+        if (g == 0) s_q2[16 * t + l16] = q2;
+      }
+    }
   }
+  // 0, or +inf or -inf whatever the score
+  const int n = NV > 0 ? NV : (nk + 63) / 64;
+  int always = 0, ordinary = nk;
+  if (rule) {
+    ordinary = 0;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const uint32_t c = NV > 0 ? of_block[NV > 0 ? i : 0] : rule_of(i);
+      always += __builtin_popcountll(__ballot(c == 1));
+      ordinary += __builtin_popcountll(__ballot(c != 1 && c != 2));
+    }
+  }
+  const bool among_always = always >= keep;  // the choice is among those alone
+  const int in = among_always ? 0 : always, all = among_always ? always : always + ordinary, W = keep < all ? keep : all;
+  auto place = [&](uint32_t c) { return c == 1 ? (among_always ? 0.f : INFINITY) : c == 2 || among_always ? -INFINITY : 0.f; };
+  float by_rule[NV > 0 ? NV : 1];
+#pragma unroll
+  for (int i = 0; i < (NV > 0 ? NV : 1); ++i) by_rule[i] = place(of_block[i]);
   __syncthreads();
-  const float k_norm = sqrtf(__uint_as_float(s_k2));
+  const float k_norm = sqrtf(__uint_as_float(wave_extreme<true>(s_k2[lane % WAVES])));
 
   for (int r = wave; r < R && first + r < nq; r += WAVES) {
-    const uint16_t* q = q0 + (long)(first + r) * DH;
     Scores<NV> v;
-    v.at = reinterpret_cast<uint32_t*>(score + (long)r * stride) + lane;
-    v.n = (nk + 63) / 64;
-    float q2 = 0.f;
-    if (lane < DH / 2) {
-      const uint32_t two = *reinterpret_cast<const uint32_t*>(q + 2 * lane);
-      const float a = __uint_as_float(two << 16), b = __uint_as_float(two & 0xffff0000u);
-      q2 = a * a + b * b;
-    }
-    const float q_norm = sqrtf(wave_sum(q2));
+    v.at = score + (long)r * stride + lane;
+    v.n = n;
+    const float q_norm = sqrtf(s_q2[r]);
     const float off = kBound * q_norm * k_norm + 7.7e-34f * (1.0f + q_norm) * (1.0f + k_norm);
-    int always = 0, free_ = 0;
-    if (rule) {
-      for (int b = lane; b < v.n * 64; b += 64) {
-        const int c = b < nk ? rule[b] : 2;
-        always += __builtin_popcountll(__ballot(c == 1));
-        free_ += __builtin_popcountll(__ballot(c != 1 && c != 2));
-      }
-    } else {
-      free_ = nk;
-    }
-    const bool among_always = always >= keep;  // the choice is among those alone
-    const int W = among_always ? keep : always + free_ < keep ? always + free_ : keep;
-    bool odd = !(off < INFINITY);  // scores that fp32 does not hold
+    const float bound = 1.01f * q_norm * k_norm + off;
+    const bool odd = !(bound < INFINITY);
+    const bool every = W == all;  // all that may be chosen are
 #pragma unroll
     for (int i = 0; i < v.count(); ++i) {
-      const int b = lane + 64 * i;
-      uint32_t x = kOut;
-      if (b < nk) {
-        const float f = score[(long)r * stride + b];
-        const int c = rule ? rule[b] : 0;
-        if (c == 1) x = among_always ? ordered(f) : kIn;
-        else if (c != 2 && !among_always) x = ordered(f);
-        if (!(fabsf(f) < INFINITY)) {
-          odd = true;
-          if (x != kOut && x != kIn) x = 1;
-        }
-      }
-      v.set(i, x);
+      const float p = NV > 0 ? by_rule[NV > 0 ? i : 0] : place(rule_of(i));
+      float f = 0.f;
+      if (!every && !odd && 64 * i < nk) f = __uint_as_float(v.at[64 * i]);
+      v.set(i, f + p);
     }
-    odd = __any(odd);
     int* to = blocks + ((long)head * nq + first + r) * keep;
-    const int some = v.how_many([](uint32_t x) { return x != kOut; });
-    if (W >= some) {
-      put_row(v, 1u, kIn, 0, to, keep, lane);
-      continue;
+    typename Scores<NV>::Border border{-3.402823466e38f, -INFINITY, W};
+    bool clear = every;
+    if (!every && !odd) {
+      border = v.border(W, in, all, bound, bound * (DH == 128 ? 0.088f : 0.125f), s_list[wave], lane);
+      clear = border.reached == W && border.least - border.next > 2.0f * off;
     }
-    if (!odd) {
-      int reached;
-      const uint32_t t = v.find(W, true, reached);
-      uint32_t least = kIn, next = kOut;  // the W-th, and what comes behind it
+    if (clear) {
+      put_row(v.count(), [&](int i) { return v.get(i) >= border.least; }, to, keep, lane);
+    } else {
 #pragma unroll
-      for (int i = 0; i < v.count(); ++i) {
-        const uint32_t x = v.get(i);
-        if (x >= t && x < least) least = x;
-        if (x < t && x > next) next = x;
-      }
-      const float last = unordered(wave_extreme<false>(least)), behind = unordered(wave_extreme<true>(next));
-      if (reached == W && last - behind > 2.0f * off) {
-        put_row(v, t, kIn, 0, to, keep, lane);
-        continue;
-      }
-      const uint32_t up = ordered(last + 2.0f * off), down = ordered(last - 2.0f * off);
-#pragma unroll
-      for (int i = 0; i < v.count(); ++i) {
-        const uint32_t x = v.get(i);
-        if (x != kOut && x != kIn) v.set(i, x > up ? kIn : x < down ? kOut : 1u);
-      }
-      if (v.how_many([](uint32_t x) { return x != kOut; }) == W) {
-        put_row(v, 1u, kIn, 0, to, keep, lane);
-        continue;
-      }
+      for (int i = 0; i < v.count(); ++i)
+        if (64 * i < nk) v.at[64 * i] = __float_as_uint(v.get(i));
+      put_row_exactly<DH>(v.at, (nk + 63) / 64, W, odd, border.least, off, s_list[wave], q0 + (long)(first + r) * DH, km, to, keep, lane);
     }
-    Scores<0> all;
-    all.at = v.at;
-    all.n = v.n;
-#pragma unroll
-    for (int i = 0; i < v.count(); ++i)
-      if (i < v.n) all.set(i, v.get(i));
-    put_row_exactly<DH>(all, W, q, km, to, keep, lane);
   }
 }
 
-// The rows of a workgroup: 16, one matrix tile, as long as their scores leave room for two workgroups on a compute unit and the launch has
-// two for each; fewer otherwise, down to one row of CHORUS_BLOCK_SELECT_MAX scores (64 KB).
+// The rows of a workgroup. All of them share one sweep over a head's keys, which at 16 rows a workgroup already is what the call waits for (1182
+// blocks of 128 values are 300 KB, from the L2), so 32 (two matrix tiles) as long as their scores fit the LDS and most compute units
+// get a workgroup; 16 and fewer otherwise, down to two rows of CHORUS_BLOCK_SELECT_MAX scores (128 KB).
 int select_rows(long nq, int H, int stride) {
-  int R = 16;
-  while (R > 1 && (size_t)R * stride * 4 > 80 * 1024) R /= 2;
-  while (R > 4 && (nq + R - 1) / R * H < 512) R /= 2;
+  int R = 32;
+  while (R > 1 && (size_t)R * stride * 4 > 155 * 1024) R /= 2;
+  while (R > 4 && (nq + R - 1) / R * H < 160) R /= 2;
   return R;
 }
 
@@ -371,24 +480,29 @@ int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_
   const int R = select_rows((long)nq, H, stride);
   const int64_t tiles = (nq + R - 1) / R;
   const size_t lds = (size_t)R * stride * sizeof(float);
-#define SELECT(DH, NV)                                                                                                                   \
+#define SELECT(DH, NV, T, THREADS)                                                                                                        \
   do {                                                                                                                                   \
     static DynLdsOnce once;                                                                                                              \
-    CHK_STATUS(once.ensure((const void*)block_select_kernel<DH, NV>, 80 * 1024));                                                        \
-    hipLaunchKernelGGL((block_select_kernel<DH, NV>), dim3((unsigned)(tiles * H)), dim3(kSelectThreads), lds, (hipStream_t)stream, Qm, Km, \
-                       rule, blocks, (int)nq, (int)nk, H / Hk, keep, R, stride, (int)tiles);                                             \
+    CHK_STATUS(once.ensure((const void*)block_select_kernel<DH, NV, T, THREADS>, 155 * 1024));                                           \
+    hipLaunchKernelGGL((block_select_kernel<DH, NV, T, THREADS>), dim3((unsigned)(tiles * H)), dim3(THREADS), lds, (hipStream_t)stream, Qm, \
+                       Km, rule, blocks, (int)nq, (int)nk, H / Hk, keep, R, stride, (int)tiles);                                         \
   } while (0)
-#define SELECT_LENGTH(DH)                  \
-  do {                                     \
-    if (nk <= 64 * 4) SELECT(DH, 4);       \
-    else if (nk <= 64 * 8) SELECT(DH, 8);  \
-    else if (nk <= 64 * 20) SELECT(DH, 20); \
-    else if (nk <= 64 * 40) SELECT(DH, 40); \
-    else SELECT(DH, 0);                    \
+#define SELECT_ROWS(DH, NV, THREADS)           \
+  do {                                         \
+    if (R == 32) SELECT(DH, NV, 2, THREADS);   \
+    else SELECT(DH, NV, 1, THREADS);           \
+  } while (0)
+#define SELECT_LENGTH(DH)                           \
+  do {                                              \
+    if (nk <= 64 * 8) SELECT_ROWS(DH, 8, 1024);     \
+    else if (nk <= 64 * 20) SELECT_ROWS(DH, 20, 1024); \
+    else if (nk <= 64 * 40) SELECT(DH, 40, 1, 512); \
+    else SELECT(DH, 0, 1, 512);                     \
   } while (0)
   if (dh == 128) SELECT_LENGTH(128);
   else SELECT_LENGTH(64);
 #undef SELECT_LENGTH
+#undef SELECT_ROWS
 #undef SELECT
   CHORUS_LAUNCH_CHECK();
   return CHORUS_OK;
