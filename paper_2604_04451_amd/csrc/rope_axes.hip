@@ -42,8 +42,10 @@ __device__ __forceinline__ float sum_squares(const float (&x)[8]) {
   return s;
 }
 
-// A wave a token; a lane takes chunks of eight values, so a head is 8 or 16 neighbouring lanes.
-template <int NORM, bool HALVES>
+// A wave a token; a lane takes chunks of eight values, so a head is 8 or 16 neighbouring lanes. HBM-bound: each row is read once and written once.
+// NCH > 0: rows of 512 NCH values, whose loads are all issued ahead of the angles and which stay in registers; NCH == 0: any number of
+// heads, chunk by chunk, and twice (the second time from the cache) where the norm is over the row.
+template <int NORM, bool HALVES, int NCH>
 __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restrict__ in, long ld, const float* __restrict__ gain,
                                                         uint16_t* __restrict__ out, long L, long Lpad, int H, int dh,
                                                         const float* __restrict__ pos, int n_axes, const double* __restrict__ freq,
@@ -58,6 +60,12 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
       *reinterpret_cast<u32x4*>(out + ((long)(c / lanes) * Lpad + row) * dh + c % lanes * 8) = u32x4{0, 0, 0, 0};
     return;
   }
+  const uint16_t* r = in + row * ld;
+  u32x4 rv[NCH > 0 ? NCH : 1];
+  if (NCH > 0) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) rv[i] = *reinterpret_cast<const u32x4*>(r + (lane + 64 * i) * 8);
+  }
   {
     float cs = 1.f, sn = 0.f;  // pairs beyond the rotated ones, or of no axis
     if (lane < n_pairs) {
@@ -71,35 +79,60 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     s_sin[wave][lane] = sn;
     __builtin_amdgcn_wave_barrier();
   }
-  const uint16_t* r = in + row * ld;
   float rstd = out_scale;
   if (NORM == CHORUS_ROPE_NORM_WIDTH) {
-    float ss = 0.f;
-    for (int c = lane; c < nchunk; c += 64) {
-      float x[8];
-      unpack8(x, *reinterpret_cast<const u32x4*>(r + c * 8));
-      ss += sum_squares(x);
+    float ss = 0.f, x[8];
+    if (NCH > 0) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        unpack8(x, rv[i]);
+        ss += sum_squares(x);
+      }
+    } else {
+      for (int c = lane; c < nchunk; c += 64) {
+        unpack8(x, *reinterpret_cast<const u32x4*>(r + c * 8));
+        ss += sum_squares(x);
+      }
     }
     rstd = rsqrtf(wave_sum(ss) / (float)(H * dh) + kEps) * out_scale;
   }
-  for (int c0 = 0; c0 < nchunk; c0 += 64) {
-    const bool live = c0 + lane < nchunk;
+  const int iters = NCH > 0 ? NCH : (nchunk + 63) / 64;
+#pragma unroll
+  for (int it = 0; it < iters; ++it) {
+    const int c0 = 64 * it;
+    const bool live = NCH > 0 || c0 + lane < nchunk;
     const int c = live ? c0 + lane : nchunk - 1;  // lanes past the end keep the head's sum company and store nothing
     const int head = c / lanes, d0 = c % lanes * 8;
     float x[8], y[8] = {};
-    unpack8(x, *reinterpret_cast<const u32x4*>(r + c * 8));
+    u32x4 u;
+    if (NCH > 0) u = rv[NCH > 0 ? it : 0];
+    else u = *reinterpret_cast<const u32x4*>(r + c * 8);
+    unpack8(x, u);
     if (NORM == CHORUS_ROPE_NORM_HEAD) rstd = rsqrtf(head_sum(sum_squares(x), lanes) / (float)dh + kEps) * out_scale;
     const float* g = NORM == CHORUS_ROPE_NORM_HEAD ? gain + d0 : gain + c * 8;
     auto scaled = [&](float(&v)[8], int off) {
+      if (NORM == CHORUS_ROPE_NORM_NONE) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= NORM == CHORUS_ROPE_NORM_NONE ? rstd : rstd * g[off + e];
+        for (int e = 0; e < 8; ++e) v[e] *= rstd;
+      } else {
+        const f32x4 g0 = *reinterpret_cast<const f32x4*>(g + off), g1 = *reinterpret_cast<const f32x4*>(g + off + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] *= rstd * g0[e];
+          v[4 + e] *= rstd * g1[e];
+        }
+      }
     };
     scaled(x, 0);
     if (HALVES) {
       const bool first = d0 < n_pairs;
-      if (d0 < 2 * n_pairs) {
-        const int off = first ? n_pairs : -n_pairs, p = first ? d0 : d0 - n_pairs;
-        unpack8(y, *reinterpret_cast<const u32x4*>(r + c * 8 + off));
+      const int off = d0 >= 2 * n_pairs ? 0 : first ? n_pairs : -n_pairs;  // where the other half of the pairs is: in a lane of the same head
+      u32x4 other;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) other[k] = __shfl(u[k], lane + off / 8, 64);
+      if (off != 0) {
+        const int p = first ? d0 : d0 - n_pairs;
+        unpack8(y, other);
         scaled(y, off);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -162,9 +195,17 @@ int32_t chorus_rope_axes(const uint16_t* in, int64_t ld, const float* gain, int3
   if (!out || !aligned16(out)) return CHORUS_E_ARG;
   if (L > 0 && (!in || !pos || (n_pairs && (!freq || !axis)) || (norm != CHORUS_ROPE_NORM_NONE && !gain))) return CHORUS_E_ARG;
   if (!aligned16(in) || !aligned16(pos) || !aligned16(freq) || !aligned16(axis) || !aligned16(gain)) return CHORUS_E_ARG;
-#define ROPE(NORM, HALVES)                                                                                                          \
-  hipLaunchKernelGGL((rope_axes_kernel<NORM, HALVES>), dim3((unsigned)((Lpad + 3) / 4)), dim3(256), 0, (hipStream_t)stream, in,     \
+  const int D = H * dh;
+#define ROPE_ROWS(NORM, HALVES, NCH)                                                                                                    \
+  hipLaunchKernelGGL((rope_axes_kernel<NORM, HALVES, NCH>), dim3((unsigned)((Lpad + 3) / 4)), dim3(256), 0, (hipStream_t)stream, in,      \
                      (long)ld, gain, out, (long)L, (long)Lpad, H, dh, pos, n_axes, freq, axis, n_pairs, out_scale)
+#define ROPE(NORM, HALVES)                              \
+  do {                                                  \
+    if (D == 512) ROPE_ROWS(NORM, HALVES, 1);           \
+    else if (D == 1536) ROPE_ROWS(NORM, HALVES, 3);     \
+    else if (D == 5120) ROPE_ROWS(NORM, HALVES, 10);    \
+    else ROPE_ROWS(NORM, HALVES, 0);                    \
+  } while (0)
 #define ROPE_LAYOUT(NORM)                                 \
   do {                                                    \
     if (layout == CHORUS_ROPE_HALVES) ROPE(NORM, true);   \
@@ -175,6 +216,7 @@ int32_t chorus_rope_axes(const uint16_t* in, int64_t ld, const float* gain, int3
   else ROPE_LAYOUT(CHORUS_ROPE_NORM_NONE);
 #undef ROPE_LAYOUT
 #undef ROPE
+#undef ROPE_ROWS
   CHORUS_LAUNCH_CHECK();
   return CHORUS_OK;
 }
