@@ -205,40 +205,77 @@ __device__ __forceinline__ void put_row(int n, TAKE take, int* __restrict__ to, 
   for (int i = put + lane; i < keep; i += 64) to[i] = -1;
 }
 
-// The choice of W where fp32 scores do not make it. It is rare, works in LDS and stays out of the row loop's registers. The row there holds
-// scores (+inf: in, -inf: out); `odd`: they say nothing, else the border is at `last`, within `off` of exact.
+// The scores within `off` of exact that the border at `last` leaves open, kMostOpen of them at most, become +inf or -inf by their exact values: 8 values of a row
+// a lane, so 8 or 16 lanes a block make its score, which is two reads and a sum away; then each open block's lane counts those in front.
+// Returns false, with nothing done, where more are open.
+constexpr int kMostOpen = 32;
+template <int DH, int NV>
+__device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float last, float off, uint64_t* __restrict__ keys, const uint16_t* __restrict__ q,
+                                             const uint16_t* __restrict__ km, int lane) {
+  const float up = last + 2.0f * off, down = last - 2.0f * off;
+  uint32_t* list = reinterpret_cast<uint32_t*>(keys);
+  int open = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < v.count(); ++i) {
+    const float x = v.get(i);
+    before += __builtin_popcountll(__ballot(x > up));
+    const uint64_t mask = __ballot(x >= down && x <= up);
+    if (mask == 0) continue;
+    const int place = lanes_below(mask, open);
+    if (mask >> lane & 1 && place < kMostOpen) list[place] = lane + 64 * i;
+    open += __builtin_popcountll(mask);
+  }
+  if (open > kMostOpen) return false;
+  __builtin_amdgcn_wave_barrier();
+  const int mine = lane < open ? (int)list[lane] : 0;
+  __builtin_amdgcn_wave_barrier();
+  constexpr int LANES = DH / 8;  // of a block
+  for (int base = 0; base < open; base += 64 / LANES) {
+    const int of = base + lane / LANES, b = __shfl(mine, of, 64);
+    const u32x4 x = *reinterpret_cast<const u32x4*>(q + lane % LANES * 8), y = *reinterpret_cast<const u32x4*>(km + (long)b * DH + lane % LANES * 8);
+    double s = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s = __builtin_fma((double)__uint_as_float(x[e] << 16), (double)__uint_as_float(y[e] << 16), s);
+      s = __builtin_fma((double)__uint_as_float(x[e] & 0xffff0000u), (double)__uint_as_float(y[e] & 0xffff0000u), s);
+    }
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d /= 2) s += __shfl_xor(s, d, 64);
+    if (lane % LANES == 0 && of < open) keys[of] = ordered(s);
+  }
+  __builtin_amdgcn_wave_barrier();
+  const uint64_t key = lane < open ? keys[lane] : 0;
+  for (int j = 0; j < open; ++j) {  // listed in ascending order of index: equal scores go to the lower lane
+    const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(key >> 32), j), lo = __builtin_amdgcn_readlane((uint32_t)key, j);
+    const uint64_t other = (uint64_t)hi << 32 | lo;
+    before += other > key || (other == key && j < lane);
+  }
+  const uint64_t kept = __ballot(lane < open && before < W);
+  __builtin_amdgcn_wave_barrier();
+  open = 0;
+#pragma unroll
+  for (int i = 0; i < v.count(); ++i) {
+    const float x = v.get(i);
+    const uint64_t mask = __ballot(x >= down && x <= up);
+    if (mask == 0) continue;
+    if (mask >> lane & 1) v.set(i, kept >> lanes_below(mask, open) & 1 ? INFINITY : -INFINITY);
+    open += __builtin_popcountll(mask);
+  }
+  return true;
+}
+
+// The choice of W where fp32 scores say nothing (`odd`), or are as good as equal by the dozen: the border is at `last`, within `off` of exact. It
+// is rare, works in LDS and stays out of the row loop's registers. The row there holds scores (+inf: in, -inf: out).
 template <int DH>
-__device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float last, float off, uint32_t* __restrict__ list,
-                                             const uint16_t* __restrict__ q, const uint16_t* __restrict__ km, int* __restrict__ to, int keep, int lane) {
-  // codes: kIn, kOut, or 1 for what the exact scores decide, the first 64 of which are listed
-  int open = 0, in = 0;
+__device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float last, float off, const uint16_t* __restrict__ q,
+                                             const uint16_t* __restrict__ km, int* __restrict__ to, int keep, int lane) {
+  // codes: kIn, kOut, or 1 for what the exact scores decide
 #pragma unroll 4
   for (int i = 0; i < n; ++i) {
     const uint32_t bits = at[64 * i];
     const float f = __uint_as_float(bits);
     const bool is_in = bits == 0x7f800000u || (!odd && f > last + 2.0f * off), is_out = bits == 0xff800000u || (!odd && f < last - 2.0f * off);
-    const uint64_t undecided = __ballot(!is_in && !is_out);
-    const int place = lanes_below(undecided, open);
     at[64 * i] = is_in ? kIn : is_out ? kOut : 1u;
-    if (!is_in && !is_out && place < 64) list[place] = lane + 64 * i;
-    in += __builtin_popcountll(__ballot(is_in));
-    open += __builtin_popcountll(undecided);
-  }
-  __builtin_amdgcn_wave_barrier();
-  // a wave that has as many lanes: each makes an exact score and counts those that come before it
-  if (open <= 64) {
-    const int b = lane < open ? list[lane] : 0;
-    const uint64_t e = lane < open ? exact_score<DH>(q, km + (long)b * DH) : 0;
-    int before = in;
-    for (int j = 0; j < open; ++j) {  // in ascending order of index: equal scores go to the lower lane
-      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(e >> 32), j), lo = __builtin_amdgcn_readlane((uint32_t)e, j);
-      const uint64_t other = (uint64_t)hi << 32 | lo;
-      before += other > e || (other == e && j < lane);
-    }
-    if (lane < open && before < W) at[b - lane] = kIn;  // `at` is this lane's first
-    __builtin_amdgcn_wave_barrier();
-    put_row(n, [&](int i) { return at[64 * i] == kIn; }, to, keep, lane);
-    return;
   }
   // the 64 bits of the scores in three parts, each among those that are alike in the part before; what is alike in all goes by index
   uint32_t from = 1, tied = kOut;
@@ -297,7 +334,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   extern __shared__ __attribute__((aligned(16))) uint32_t score[];  // [R][stride]
   __shared__ uint32_t s_k2[WAVES];        // the largest squared norm of a block of keys that a wave met
   __shared__ float s_q2[16 * T];          // the rows' squared norms
-  __shared__ uint32_t s_list[WAVES][64];  // scores at a border, and blocks that the fp32 scores leave open
+  __shared__ uint64_t s_list[WAVES][kMostOpen];  // 64 scores at a border, then the exact ones of the blocks that are open
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int at = xcd_remap(blockIdx.x, gridDim.x), head = at / tiles, first = (at - head * tiles) * R;
   const uint16_t* q0 = Qm + (long)head * nq * DH;
@@ -417,19 +454,26 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
       v.set(i, f + p);
     }
     int* to = blocks + ((long)head * nq + first + r) * keep;
+    const uint16_t* q = q0 + (long)(first + r) * DH;
     typename Scores<NV>::Border border{-3.402823466e38f, -INFINITY, W};
+    float from = border.least;
     bool clear = every;
     if (!every && !odd) {
-      border = v.border(W, in, all, bound, bound * (DH == 128 ? 0.088f : 0.125f), s_list[wave], lane);
+      border = v.border(W, in, all, bound, bound * (DH == 128 ? 0.088f : 0.125f), reinterpret_cast<uint32_t*>(s_list[wave]), lane);
       clear = border.reached == W && border.least - border.next > 2.0f * off;
+      from = border.least;
+      if (!clear) {
+        clear = close_border<DH>(v, W, border.least, off, s_list[wave], q, km, lane);
+        from = border.least + 2.0f * off;  // nothing is between this and what was open
+      }
     }
     if (clear) {
-      put_row(v.count(), [&](int i) { return v.get(i) >= border.least; }, to, keep, lane);
+      put_row(v.count(), [&](int i) { return v.get(i) >= from; }, to, keep, lane);
     } else {
 #pragma unroll
       for (int i = 0; i < v.count(); ++i)
         if (64 * i < nk) v.at[64 * i] = __float_as_uint(v.get(i));
-      put_row_exactly<DH>(v.at, (nk + 63) / 64, W, odd, border.least, off, s_list[wave], q0 + (long)(first + r) * DH, km, to, keep, lane);
+      put_row_exactly<DH>(v.at, (nk + 63) / 64, W, odd, border.least, off, q, km, to, keep, lane);
     }
   }
 }
