@@ -51,30 +51,26 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
 // How far a score can be off: products of bf16 are exact in fp32, and whatever the order of a sum of DH <= 128 of them, each of its
 // additions is off by at most 2^-23 of the sum of magnitudes, itself at most |q| |k|: kBound |q| max |k|, and a trace for values
 // that are flushed. Norms come from the same pipe (the diagonal of K K^T) and are within 2^-16 of their values, which kBound has room for.
-// Where that bound is finite so is every score; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
+// Where |q| |k| is a number below 1e38 every score is one; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
 //
-// Bound by the vector pipe: a row of 1182 blocks costs about 500 instructions of its wave, 20 of them for each look at all its scores. The fast
-// path therefore stays in floats: a block that is in whatever its score (`always`) scores +inf, one that is out -inf.
+// Half of a workgroup's time goes into the sweep over the keys, half into its rows; there the vector and the scalar pipe share the work, 20
+// comparisons and 40 counts for each look at the scores of 1182 blocks. The search therefore stays in floats, with no more than a mean
+// between two looks (compared and bisected as integers, for a sure end: 114 us and 21.5 instead of 92 and 17): a block that is in whatever its score
+// (`always`) scores +inf, one that is out -inf.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kIn = 0xffffffffu, kOut = 0u;  // the same two as codes: no finite float has them
 constexpr float kBound = 1.05f / 65536.0f;
+constexpr float kTrace = 2e-36f;  // more than 128 squares that fp32 does not hold
 
-// Codes: 32 bits whose unsigned order is the order of the floats, both zeros alike.
-__device__ __forceinline__ uint32_t ordered(float f) {
-  const uint32_t b = __float_as_uint(f + 0.0f);
-  return b >> 31 ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float unordered(uint32_t v) { return __uint_as_float(v >> 31 ? v & 0x7fffffffu : ~v); }
-// NaN below every number
+// A score as 64 bits whose unsigned order is that of the scores: both zeros alike, NaN below every number.
 __device__ __forceinline__ uint64_t ordered(double s) {
   if (s != s) return 0;
   const uint64_t b = __builtin_bit_cast(uint64_t, s + 0.0);
   return b >> 63 ? ~b : b | (1ull << 63);
 }
 
-template <bool MAX>
-__device__ __forceinline__ uint32_t wave_extreme(uint32_t v) {
-  auto of = [](uint32_t a, uint32_t b) { return (a > b) == MAX ? a : b; };
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  auto of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
   const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   v = of(h[0], h[1]);
   const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
@@ -122,72 +118,64 @@ struct Scores {
     for (int i = 0; i < count(); ++i) c += __builtin_popcountll(__ballot(get(i) >= t));
     return c;
   }
-  // The border of the W largest, `in` of them +inf and `all` not -inf: the least of them, the next one behind, and how many reach the former (more than
-  // W where several are equal). Bisection between -bound and bound, beyond which there are finite scores on neither side: first at twice the
-  // usual size of a score and at 0, then of the values for a while (a row's scores are spread like a bell, and halves of their range
-  // come near in a few steps, as halves of the order of their bits do not), then of the order, which always ends. As soon as the border lies
-  // among 64 scores or fewer they move to a lane each, and a step costs one comparison.
+  // Where the border of the W largest is, `in` of the scores being +inf and `all` not -inf: `reached` of them reach `low`, W or more, and fewer than W
+  // lie above `high`. Bisection between -bound and bound, beyond which there are finite scores on neither side: first at twice the usual
+  // size of a score and at 0, then in the middle (a row's scores are spread like a bell, and halves of their range come near in a few
+  // steps), until W are left above, or no more is to be had from scores that are `off` from exact. As soon as the border lies among 64 scores
+  // or fewer they move to a lane each, and a step costs one comparison. With W reached low = high is the W-th score, and `next` the one behind.
   struct Border {
-    float least, next;
+    float low, high, next;
     int reached;
   };
-  __device__ __forceinline__ Border border(int W, int in, int all, float bound, float usual, uint32_t* __restrict__ list, int lane) const {
-    uint32_t lo = __builtin_amdgcn_readfirstlane(ordered(-bound)), hi = __builtin_amdgcn_readfirstlane(ordered(bound)) + 1;
-    auto middle = [&](int step) {
-      const float half = step == 0 ? 2.0f * usual : step == 1 ? 0.f : 0.5f * unordered(lo) + 0.5f * unordered(hi);
-      const uint32_t m = __builtin_amdgcn_readfirstlane(ordered(half));
-      return step < 18 && m > lo && m < hi ? m : lo + (hi - lo) / 2;
-    };
-    int reach_lo = all, reach_hi = in, step = 0;
-    for (; reach_lo != W && hi - lo > 1 && reach_lo - reach_hi > 64; ++step) {
-      const uint32_t mid = middle(step);
-      const int c = reach(unordered(mid));
-      if (c >= W) {
-        lo = mid;
-        reach_lo = c;
-      } else {
-        hi = mid;
-        reach_hi = c;
-      }
+  __device__ __forceinline__ Border border(int W, int in, int all, float bound, float usual, float off, float* __restrict__ list, int lane) const {
+    float lo = -bound, hi = 1.01f * bound;
+    int reach_lo = all, reach_hi = in;
+    float mid = 2.0f * usual;
+    while (reach_lo != W && hi - lo > off && reach_lo - reach_hi > 64) {
+      const int c = reach(mid);
+      const bool low = c >= W;
+      reach_lo = low ? c : reach_lo;
+      reach_hi = low ? reach_hi : c;
+      lo = low ? mid : lo;
+      hi = low ? hi : mid;
+      mid = lo < 0.f && hi == 2.0f * usual ? 0.f : 0.5f * lo + 0.5f * hi;
     }
-    const float from = unordered(lo), to = unordered(hi);
     float least = INFINITY, next = -INFINITY;
-    if (reach_lo == W || hi - lo <= 1) {
+    if (reach_lo == W) {
 #pragma unroll
       for (int i = 0; i < count(); ++i) {
         const float x = get(i);
-        least = fminf(least, x >= from ? x : INFINITY);
-        next = fmaxf(next, x >= from ? -INFINITY : x);
+        least = fminf(least, x >= lo ? x : INFINITY);
+        next = fmaxf(next, x >= lo ? -INFINITY : x);
       }
-    } else {
+    } else if (reach_lo - reach_hi <= 64) {
       int at = 0;
 #pragma unroll
       for (int i = 0; i < count(); ++i) {
         const float x = get(i);
-        const bool of = x >= from && x < to;
+        const bool of = x >= lo && x < hi;
         const uint64_t taken = __ballot(of);
-        if (of) list[lanes_below(taken, at)] = __float_as_uint(x);
+        if (of) list[lanes_below(taken, at)] = x;
         at += __builtin_popcountll(taken);
       }
       __builtin_amdgcn_wave_barrier();
-      const float x = lane < at ? __uint_as_float(list[lane]) : -INFINITY;
-      const uint32_t code = ordered(x);
-      for (; reach_lo != W && hi - lo > 1; ++step) {
-        const uint32_t mid = middle(step);
-        const int c = reach_hi + __builtin_popcountll(__ballot(code >= mid && code < hi));
-        if (c >= W) {
-          lo = mid;
-          reach_lo = c;
-        } else {
-          hi = mid;
-          reach_hi = c;
-        }
-      }
-      least = code >= lo ? x : INFINITY;
-      next = code < lo ? x : -INFINITY;
+      const float x = lane < at ? list[lane] : -INFINITY;
       __builtin_amdgcn_wave_barrier();
+      const int above = reach_hi;
+      while (reach_lo != W && hi - lo > off) {
+        mid = 0.5f * lo + 0.5f * hi;
+        const int c = above + __builtin_popcountll(__ballot(x >= mid));
+        const bool low = c >= W;
+        reach_lo = low ? c : reach_lo;
+        lo = low ? mid : lo;
+        hi = low ? hi : mid;
+      }
+      least = x >= lo ? x : INFINITY;
+      next = x < lo ? x : -INFINITY;
     }
-    return Border{unordered(wave_extreme<false>(ordered(least))), unordered(wave_extreme<true>(ordered(next))), reach_lo};
+    if (reach_lo != W) return Border{lo, hi, lo, reach_lo};
+    least = -wave_max(-least);
+    return Border{least, least, wave_max(next), W};
   }
 };
 
@@ -205,14 +193,13 @@ __device__ __forceinline__ void put_row(int n, TAKE take, int* __restrict__ to, 
   for (int i = put + lane; i < keep; i += 64) to[i] = -1;
 }
 
-// The scores within `off` of exact that the border at `last` leaves open, kMostOpen of them at most, become +inf or -inf by their exact values: 8 values of a row
+// The scores from `down` to `up`, which the others leave open, kMostOpen of them at most, become +inf or -inf by their exact values: 8 values of a row
 // a lane, so 8 or 16 lanes a block make its score, which is two reads and a sum away; then each open block's lane counts those in front.
 // Returns false, with nothing done, where more are open.
 constexpr int kMostOpen = 32;
 template <int DH, int NV>
-__device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float last, float off, uint64_t* __restrict__ keys, const uint16_t* __restrict__ q,
+__device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float down, float up, uint64_t* __restrict__ keys, const uint16_t* __restrict__ q,
                                              const uint16_t* __restrict__ km, int lane) {
-  const float up = last + 2.0f * off, down = last - 2.0f * off;
   uint32_t* list = reinterpret_cast<uint32_t*>(keys);
   int open = 0, before = 0;
 #pragma unroll
@@ -264,17 +251,16 @@ __device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float last, f
   return true;
 }
 
-// The choice of W where fp32 scores say nothing (`odd`), or are as good as equal by the dozen: the border is at `last`, within `off` of exact. It
-// is rare, works in LDS and stays out of the row loop's registers. The row there holds scores (+inf: in, -inf: out).
+// The choice of W where fp32 scores say nothing (`odd`), or are as good as equal by the dozen, from `down` to `up`. It is rare, works in LDS and stays out of the row loop's registers. The row there holds scores (+inf: in, -inf: out).
 template <int DH>
-__device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float last, float off, const uint16_t* __restrict__ q,
+__device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float down, float up, const uint16_t* __restrict__ q,
                                              const uint16_t* __restrict__ km, int* __restrict__ to, int keep, int lane) {
   // codes: kIn, kOut, or 1 for what the exact scores decide
 #pragma unroll 4
   for (int i = 0; i < n; ++i) {
     const uint32_t bits = at[64 * i];
     const float f = __uint_as_float(bits);
-    const bool is_in = bits == 0x7f800000u || (!odd && f > last + 2.0f * off), is_out = bits == 0xff800000u || (!odd && f < last - 2.0f * off);
+    const bool is_in = bits == 0x7f800000u || (!odd && f > up), is_out = bits == 0xff800000u || (!odd && f < down);
     at[64 * i] = is_in ? kIn : is_out ? kOut : 1u;
   }
   // the 64 bits of the scores in three parts, each among those that are alike in the part before; what is alike in all goes by index
@@ -400,7 +386,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
       fetch(kf[1], strip + 4 * WAVES);
       use(kf[2], strip + 2 * WAVES);
     }
-    k2 = wave_extreme<true>(g == l16 >> 2 ? k2 : 0);
+    k2 = wave_max_u32(g == l16 >> 2 ? k2 : 0);
     if (lane == 0) s_k2[wave] = k2;
     if (wave == 0) {
 #pragma unroll
@@ -435,16 +421,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
 #pragma unroll
   for (int i = 0; i < (NV > 0 ? NV : 1); ++i) by_rule[i] = place(of_block[i]);
   __syncthreads();
-  const float k_norm = sqrtf(__uint_as_float(wave_extreme<true>(s_k2[lane % WAVES])));
+  const float k_norm = sqrtf(__uint_as_float(wave_max_u32(s_k2[lane % WAVES])) + kTrace);
 
   for (int r = wave; r < R && first + r < nq; r += WAVES) {
     Scores<NV> v;
     v.at = score + (long)r * stride + lane;
     v.n = n;
-    const float q_norm = sqrtf(s_q2[r]);
+    const float q_norm = sqrtf(__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_q2[r]))) + kTrace);
     const float off = kBound * q_norm * k_norm + 7.7e-34f * (1.0f + q_norm) * (1.0f + k_norm);
     const float bound = 1.01f * q_norm * k_norm + off;
-    const bool odd = !(bound < INFINITY);
+    const bool odd = !(bound < 1e38f);  // room for a search between -bound and a little more than bound
     const bool every = W == all;  // all that may be chosen are
 #pragma unroll
     for (int i = 0; i < v.count(); ++i) {
@@ -455,16 +441,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
     }
     int* to = blocks + ((long)head * nq + first + r) * keep;
     const uint16_t* q = q0 + (long)(first + r) * DH;
-    typename Scores<NV>::Border border{-3.402823466e38f, -INFINITY, W};
-    float from = border.least;
+    float from = -3.402823466e38f, down = 0.f;
     bool clear = every;
     if (!every && !odd) {
-      border = v.border(W, in, all, bound, bound * (DH == 128 ? 0.088f : 0.125f), reinterpret_cast<uint32_t*>(s_list[wave]), lane);
-      clear = border.reached == W && border.least - border.next > 2.0f * off;
-      from = border.least;
+      const auto border = v.border(W, in, all, bound, bound * (DH == 128 ? 0.088f : 0.125f), off, reinterpret_cast<float*>(s_list[wave]), lane);
+      from = border.low;
+      clear = border.reached == W && border.low - border.next > 2.0f * off;
       if (!clear) {
-        clear = close_border<DH>(v, W, border.least, off, s_list[wave], q, km, lane);
-        from = border.least + 2.0f * off;  // nothing is between this and what was open
+        down = border.low - 2.0f * off;
+        from = border.high + 2.0f * off;  // nothing is left between `down` and this
+        clear = close_border<DH>(v, W, down, from, s_list[wave], q, km, lane);
       }
     }
     if (clear) {
@@ -473,7 +459,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
 #pragma unroll
       for (int i = 0; i < v.count(); ++i)
         if (64 * i < nk) v.at[64 * i] = __float_as_uint(v.get(i));
-      put_row_exactly<DH>(v.at, (nk + 63) / 64, W, odd, border.least, off, q, km, to, keep, lane);
+      put_row_exactly<DH>(v.at, (nk + 63) / 64, W, odd, down, from, q, km, to, keep, lane);
     }
   }
 }

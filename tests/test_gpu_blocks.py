@@ -229,6 +229,18 @@ def test_block_select_neighbours_closer_than_fp32():
     np.testing.assert_array_equal(out.cpu().numpy(), OB.block_select(Qm, Km, keep))
 
 
+@pytest.mark.parametrize("q_scale,k_scale", [(1.0, 1e-30), (1e-20, 1e-18), (1.0, 1e-39), (1e18, 1e18), (3e18, 3e18), (1e19, 1e19), (1.0, 1e38), (1e-30, 3e38), (0.0, 1.0)])
+def test_block_select_far_scales(q_scale, k_scale):
+    """Scores that fp32 does not hold, barely holds or flushes, and scores that are all zero: fp64 decides."""
+    print(f"[case] block_select scales {q_scale} {k_scale}", flush=True)
+    rng = np.random.default_rng(17)
+    Qm = _bf(np.clip(rng.standard_normal((2, 5, 128)) / 3, -1, 1) * q_scale)
+    Km = _bf(np.clip(rng.standard_normal((2, 300, 128)) / 3, -1, 1) * k_scale)
+    out = torch.empty(2, 5, 40, dtype=torch.int32, device=DEV)
+    B.chorus_block_select(dev_bf16(Qm), dev_bf16(Km), out)
+    np.testing.assert_array_equal(out.cpu().numpy(), OB.block_select(Qm, Km, 40))
+
+
 # ------------------------------------------------------------------------------------------------ means, rotations
 
 @pytest.mark.parametrize("H,dh,L,block", [(1, 64, 1, 64), (2, 128, 63, 64), (3, 64, 64, 128), (2, 128, 129, 128), (5, 64, 1000, 64),
