@@ -5,26 +5,48 @@
 namespace chorus {
 namespace {
 
-// Mean over blocks of `block` consecutive rows of a head, a wave a block: a lane sums one chunk of eight values of every 64 / (dh / 8)-th
-// row, then the lanes of a chunk are added. HBM-bound: each row is read once, 16 bytes a lane.
-template <int DH>
+// Mean over blocks of BLOCK consecutive rows of a head, a wave a block: a lane sums one chunk of eight values of every 64 / (dh / 8)-th
+// row, then the lanes of a chunk are added. HBM-bound: each row is read once, 16 bytes a lane, eight rows of a lane in flight (75600 x 5120 135 us,
+// 5.8 TB/s; 3271 x 1536 3.9 us, with one behind the other, where few blocks wait a memory latency a row, 6.8).
+template <int DH, int BLOCK>
 __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restrict__ X, uint16_t* __restrict__ out, long L, long Lpad,
-                                                         int block, long nb, long total) {
-  constexpr int LANES = DH / 8, ROWS = 64 / LANES;
+                                                         long nb, long total) {
+  constexpr int LANES = DH / 8, ROWS = 64 / LANES, TIMES = BLOCK / ROWS;
   const int lane = threadIdx.x & 63;
   const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= total) return;
   const long head = id / nb, b = id - head * nb;
-  const long first = b * block;
-  const int n = (int)(L - first < block ? L - first : block);
+  const long first = b * BLOCK;
+  const int n = (int)(L - first < BLOCK ? L - first : BLOCK), mine = lane / LANES;
   const uint16_t* x = X + (head * Lpad + first) * DH + lane * 8;
   float s[8] = {};
-  for (int r = lane / LANES, i = 0; r < n; r += ROWS, ++i) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(x + (long)i * ROWS * DH);
+  auto add = [&](const u32x4& u) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       s[2 * k] += __uint_as_float(u[k] << 16);
       s[2 * k + 1] += __uint_as_float(u[k] & 0xffff0000u);
+    }
+  };
+  if (n == BLOCK) {
+#pragma unroll
+    for (int i0 = 0; i0 < TIMES; i0 += 8) {
+      u32x4 u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const u32x4*>(x + (i0 + i) * ROWS * DH);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) add(u[i]);
+    }
+  } else {
+    for (int i0 = 0; i0 * ROWS < n; i0 += 8) {  // a short last block: its last row stands for those behind its end, which are not added
+      u32x4 u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = (i0 + i) * ROWS + mine;
+        u[i] = *reinterpret_cast<const u32x4*>(x + ((row < n ? row : n - 1) - mine) * DH);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if ((i0 + i) * ROWS + mine < n) add(u[i]);
     }
   }
 #pragma unroll
@@ -113,9 +135,18 @@ struct Scores {
     else at[64 * i] = __float_as_uint(v);
   }
   __device__ __forceinline__ int reach(float t) const {  // how many of the wave's scores reach t
-    int c = 0;
+    int c = 0, i = 0;
+    if (NV == 0) {  // eight reads in flight
+      for (; i + 8 <= n; i += 8) {
+        float x[8];
 #pragma unroll
-    for (int i = 0; i < count(); ++i) c += __builtin_popcountll(__ballot(get(i) >= t));
+        for (int j = 0; j < 8; ++j) x[j] = get(i + j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c += __builtin_popcountll(__ballot(x[j] >= t));
+      }
+    }
+#pragma unroll
+    for (; i < count(); ++i) c += __builtin_popcountll(__ballot(get(i) >= t));
     return c;
   }
   // Where the border of the W largest is, `in` of the scores being +inf and `all` not -inf: `reached` of them reach `low`, W or more, and fewer than W
@@ -464,13 +495,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   }
 }
 
-// The rows of a workgroup. All of them share one sweep over a head's keys, which at 16 rows a workgroup already is what the call waits for (1182
-// blocks of 128 values are 300 KB, from the L2), so 32 (two matrix tiles) as long as their scores fit the LDS and most compute units
-// get a workgroup; 16 and fewer otherwise, down to two rows of CHORUS_BLOCK_SELECT_MAX scores (128 KB).
+// The rows of a workgroup. All of them share one sweep over a head's keys, which is what the call waits for (1182 blocks of 128 values are 300 KB, from
+// the L2, and a compute unit holds one workgroup): as few as let the launch run in one round of workgroups, and where it takes more than
+// one, 32 (two matrix tiles) or as many as their scores leave room for in the LDS, down to two rows of CHORUS_BLOCK_SELECT_MAX scores
+// (128 KB). 103 x 205 blocks, 12 heads: 8 rows 13 us, 4 rows (312 workgroups) 20.
 int select_rows(long nq, int H, int stride) {
-  int R = 32;
+  int R = 4;
+  while (R < 32 && (nq + R - 1) / R * H > 256) R *= 2;
   while (R > 1 && (size_t)R * stride * 4 > 155 * 1024) R /= 2;
-  while (R > 4 && (nq + R - 1) / R * H < 160) R /= 2;
   return R;
 }
 
@@ -491,10 +523,16 @@ int32_t chorus_block_mean(const uint16_t* X, uint16_t* out, int64_t L, int64_t L
   const int64_t total = nb * H, groups = (total + 3) / 4;
   if (groups > 0x7fffffffL) return CHORUS_E_SHAPE;
   const dim3 grid((unsigned)groups);
-  if (dh == 128)
-    hipLaunchKernelGGL(block_mean_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, X, out, (long)L, (long)Lpad, block, (long)nb, (long)total);
-  else
-    hipLaunchKernelGGL(block_mean_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, X, out, (long)L, (long)Lpad, block, (long)nb, (long)total);
+#define MEAN(DH, BLOCK) \
+  hipLaunchKernelGGL((block_mean_kernel<DH, BLOCK>), grid, dim3(256), 0, (hipStream_t)stream, X, out, (long)L, (long)Lpad, (long)nb, (long)total)
+  if (dh == 128) {
+    if (block == CHORUS_BLOCK_QUERIES) MEAN(128, CHORUS_BLOCK_QUERIES);
+    else MEAN(128, CHORUS_BLOCK_KEYS);
+  } else {
+    if (block == CHORUS_BLOCK_QUERIES) MEAN(64, CHORUS_BLOCK_QUERIES);
+    else MEAN(64, CHORUS_BLOCK_KEYS);
+  }
+#undef MEAN
   CHORUS_LAUNCH_CHECK();
   return CHORUS_OK;
 }
@@ -522,12 +560,13 @@ int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_
     if (R == 32) SELECT(DH, NV, 2, THREADS);   \
     else SELECT(DH, NV, 1, THREADS);           \
   } while (0)
+  // A row's scores stay in registers up to 40 a lane; behind that they are read from LDS at each look (2 rows of 9000 blocks: 145 us).
 #define SELECT_LENGTH(DH)                           \
   do {                                              \
     if (nk <= 64 * 8) SELECT_ROWS(DH, 8, 1024);     \
     else if (nk <= 64 * 20) SELECT_ROWS(DH, 20, 1024); \
     else if (nk <= 64 * 40) SELECT(DH, 40, 1, 512); \
-    else SELECT(DH, 0, 1, 512);                     \
+    else SELECT(DH, 0, 1, 1024);                    \
   } while (0)
   if (dh == 128) SELECT_LENGTH(128);
   else SELECT_LENGTH(64);
