@@ -187,7 +187,7 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
  *   fp64, NaN below every number, the higher first, equal ones by ascending index
  *   rule   dev uint8 [nk] or NULL: 1 = ahead of all others, 2 = never, anything else by its score
  *   blocks dev int32 [H, nq, keep]: ascending, -1 behind the last
- *   nk from 1 to CHORUS_BLOCK_SELECT_MAX (CHORUS_E_SHAPE), keep >= 1.
+ *   nk from 1 to CHORUS_BLOCK_SELECT_MAX, nq * H at most 2^22 - 1 (CHORUS_E_SHAPE), keep >= 1.
  *
  * chorus_attention_blocks: O = softmax(Q K^T / sqrt(dh)) V with the queries of block a (CHORUS_BLOCK_QUERIES of them) of head h seeing
  *   the keys of the key blocks (CHORUS_BLOCK_KEYS keys) in blocks[h, a, :] only. An entry outside [0, ceil(Lk / 64)) is passed over, so
@@ -196,8 +196,10 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
  *   Q dev bf16 [H, LqPad, dh], K dev bf16 [Hk, LkPad, dh], Vt dev bf16 [Hk*dh, LkPad] in chorus_v_transpose's layout
  *   (H % Hk == 0; head h reads h / (H / Hk)), O dev bf16 [Lq, H*dh], blocks dev int32 [H, ceil(Lq / 128), keep]
  *   prescaled  non-zero: Q holds the queries multiplied by CHORUS_ATTENTION_Q_PRESCALE(dh), as for chorus_attention's variant 6
- *   ws    dev, chorus_attention_blocks_workspace_bytes bytes (0: none, ws may be NULL)
- *   dh in {64,128}; LkPad % 64 == 0, LkPad >= Lk >= 1; rows and columns beyond Lq and Lk are padding (finite values).
+ *   ws    dev, chorus_attention_blocks_workspace_bytes bytes (0: none, ws may be NULL): the fp32 results of lists that are cut so that few
+ *         of them fill the GPU. Scratch of this call alone: calls that may run at the same time need one each
+ *   dh in {64,128}; LkPad % 64 == 0, 2^22 >= LkPad >= Lk >= 1; at most 2^24 - 2^15 - 2 lists (H * ceil(Lq / 128)); rows and columns
+ *   beyond Lq and Lk are padding (finite values).
  * Errors: CHORUS_E_ARG, CHORUS_E_SHAPE, CHORUS_E_WORKSPACE, CHORUS_E_HIP.
  * ------------------------------------------------------------------------ */
 #define CHORUS_ROPE_NORM_NONE 0

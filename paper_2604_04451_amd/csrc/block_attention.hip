@@ -26,6 +26,7 @@ namespace {
 constexpr int BQ = CHORUS_BLOCK_QUERIES, BK = CHORUS_BLOCK_KEYS;
 constexpr int64_t kMostKeys = 1 << 22;  // a head's keys and values in bytes stay within the 32-bit offsets of the loads
 constexpr int kMostSlices = 64;         // the join holds a slice a lane
+constexpr int64_t kMostLists = (1 << 24) - 512 * kMostSlices - 2;  // with the last round's slices, 256 threads each, within the 2^32 of a launch
 
 // How a launch goes: the first `whole` lists by one half of a workgroup each, the others cut into `slices` (entry e of a list goes to slice
 // e % slices, so that a short list with its end full of -1 is cut evenly), whose results are joined by a second launch.
@@ -412,7 +413,7 @@ extern "C" {
 size_t chorus_attention_blocks_workspace_bytes(int64_t Lq, int32_t H, int32_t dh, int32_t keep) {
   if (Lq <= 0 || H <= 0 || (dh != 64 && dh != 128) || keep < 1 || Lq > 0x7fffffffL) return 0;
   const int64_t nq = (Lq + BQ - 1) / BQ;
-  return nq > 0x7fffffffL / H ? 0 : plan_bytes(block_plan((long)(nq * H), dh, keep), dh);
+  return nq > kMostLists / H ? 0 : plan_bytes(block_plan((long)(nq * H), dh, keep), dh);
 }
 
 int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint16_t* Vt, uint16_t* O, const int32_t* blocks, int32_t keep,
@@ -422,7 +423,7 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
   if ((dh != 64 && dh != 128) || H % Hk || Lk < 1 || LkPad % BK || LkPad > kMostKeys) return CHORUS_E_SHAPE;
   if (Lq > 0x7fffffffL) return CHORUS_E_SHAPE;
   const int64_t nq = (Lq + BQ - 1) / BQ, nk = (Lk + BK - 1) / BK;
-  if (nq > (0x7fffffffL - kMostSlices * 512) / H) return CHORUS_E_SHAPE;
+  if (nq > kMostLists / H || keep > 0x7fffffff - kMostSlices) return CHORUS_E_SHAPE;
   if (Lq == 0) return CHORUS_OK;
   if (!Q || !K || !Vt || !O || !blocks) return CHORUS_E_ARG;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(Vt) || !aligned16(O) || !aligned16(blocks) || !aligned16(ws)) return CHORUS_E_ARG;

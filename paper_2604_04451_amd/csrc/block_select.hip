@@ -6,7 +6,7 @@ namespace chorus {
 namespace {
 
 // Mean over blocks of BLOCK consecutive rows of a head, a wave a block: a lane sums one chunk of eight values of every 64 / (dh / 8)-th
-// row, then the lanes of a chunk are added. HBM-bound: each row is read once, 16 bytes a lane, eight rows of a lane in flight (75600 x 5120 135 us,
+// row, each divided by BLOCK ahead of the sum, which is exact and keeps sums of the largest values finite, then the lanes of a chunk are added. HBM-bound: each row is read once, 16 bytes a lane, eight rows of a lane in flight (75600 x 5120 135 us,
 // 5.8 TB/s; 3271 x 1536 3.9 us, with one behind the other, where few blocks wait a memory latency a row, 6.8).
 template <int DH, int BLOCK>
 __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restrict__ X, uint16_t* __restrict__ out, long L, long Lpad,
@@ -23,8 +23,8 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
   auto add = [&](const u32x4& u) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      s[2 * k] += __uint_as_float(u[k] << 16);
-      s[2 * k + 1] += __uint_as_float(u[k] & 0xffff0000u);
+      s[2 * k] = __builtin_fmaf(__uint_as_float(u[k] << 16), 1.0f / BLOCK, s[2 * k]);
+      s[2 * k + 1] = __builtin_fmaf(__uint_as_float(u[k] & 0xffff0000u), 1.0f / BLOCK, s[2 * k + 1]);
     }
   };
   if (n == BLOCK) {
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
   if (lane < LANES) {
     u32x4 o;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = pack_bf16x2(s[2 * k] / (float)n, s[2 * k + 1] / (float)n);
+    for (int k = 0; k < 4; ++k) o[k] = pack_bf16x2(s[2 * k] / (float)n * BLOCK, s[2 * k + 1] / (float)n * BLOCK);
     *reinterpret_cast<u32x4*>(out + (head * nb + b) * DH + lane * 8) = o;
   }
 }
@@ -518,10 +518,10 @@ int32_t chorus_block_mean(const uint16_t* X, uint16_t* out, int64_t L, int64_t L
   if ((dh != 64 && dh != 128) || (block != CHORUS_BLOCK_QUERIES && block != CHORUS_BLOCK_KEYS)) return CHORUS_E_SHAPE;
   if (L == 0) return CHORUS_OK;
   if (!X || !out || !aligned16(X) || !aligned16(out)) return CHORUS_E_ARG;
-  const int64_t nb = (L + block - 1) / block;
+  const int64_t nb = L / block + (L % block != 0);
   if (nb > 0x7fffffffL) return CHORUS_E_SHAPE;
   const int64_t total = nb * H, groups = (total + 3) / 4;
-  if (groups > 0x7fffffffL) return CHORUS_E_SHAPE;
+  if (groups > 0xffffffffL / 256) return CHORUS_E_SHAPE;  // the threads of a launch
   const dim3 grid((unsigned)groups);
 #define MEAN(DH, BLOCK) \
   hipLaunchKernelGGL((block_mean_kernel<DH, BLOCK>), grid, dim3(256), 0, (hipStream_t)stream, X, out, (long)L, (long)Lpad, (long)nb, (long)total)
@@ -541,7 +541,8 @@ int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_
                             int32_t Hk, int32_t dh, int32_t keep, void* stream) {
   if (nq < 0 || nk < 0 || H <= 0 || Hk <= 0 || keep < 1) return CHORUS_E_ARG;
   if (H % Hk || (dh != 64 && dh != 128) || nk < 1 || nk > CHORUS_BLOCK_SELECT_MAX) return CHORUS_E_SHAPE;
-  if (nq > 0x7fffffffL / H) return CHORUS_E_SHAPE;
+  // a workgroup of up to 1024 threads for each row at the most, of the 2^32 - 1 of a launch
+  if (nq > 0xffffffffL / 1024 / H || keep > 0x7fffffff - 64) return CHORUS_E_SHAPE;
   if (nq == 0) return CHORUS_OK;
   if (!Qm || !Km || !blocks || !aligned16(Qm) || !aligned16(Km) || !aligned16(blocks) || !aligned16(rule)) return CHORUS_E_ARG;
   const int stride = (int)((nk + 63) / 64 * 64) + 4;  // rows 4 banks apart

@@ -194,7 +194,7 @@ int32_t chorus_rope_axes(const uint16_t* in, int64_t ld, const float* gain, int3
   if (!(out_scale > 0.f) || !(out_scale < INFINITY)) return CHORUS_E_ARG;
   if ((dh != 64 && dh != 128) || H > (1 << 20) || 2 * (int64_t)n_pairs > dh) return CHORUS_E_SHAPE;
   if (layout == CHORUS_ROPE_HALVES && n_pairs % 8) return CHORUS_E_SHAPE;
-  if (ld % 8 || ld < (int64_t)H * dh || (Lpad + 3) / 4 > 0x7fffffffL) return CHORUS_E_SHAPE;
+  if (ld % 8 || ld < (int64_t)H * dh || Lpad > 0xffffffffL / 64 - 3) return CHORUS_E_SHAPE;  // 64 threads a row, of the 2^32 - 1 of a launch
   if (Lpad == 0) return CHORUS_OK;
   if (!out || !aligned16(out)) return CHORUS_E_ARG;
   if (L > 0 && (!in || !pos || (n_pairs && (!freq || !axis)) || (norm != CHORUS_ROPE_NORM_NONE && !gain))) return CHORUS_E_ARG;

@@ -90,6 +90,18 @@ def test_attention_blocks_workspace():
     assert need(1 << 40, 4, 64, 100) == need((1 << 31) - 1, 1 << 20, 64, 100) == 0
 
 
+def test_refuses_more_than_a_launch_holds():
+    """Rows, lists and entries whose number does not fit a launch or 32 bits are refused, lengths at the end of 64 bits included."""
+    lib, most = P.load(), (1 << 63) - 1
+    for Lpad in ((1 << 26), most - 2, most):
+        assert _rope(lib, Lpad=Lpad) == B.E_SHAPE
+    assert _mean(lib, L=1, Lpad=1, H=1 << 26) == _mean(lib, L=most, Lpad=most) == B.E_SHAPE
+    assert _select(lib, nq=1, H=1 << 30, Hk=1) == _select(lib, nq=1 << 28) == _select(lib, nq=most) == _select(lib, keep=(1 << 31) - 1) == B.E_SHAPE
+    ws = dict(ws=P16, ws_bytes=1 << 62)
+    assert _attend(lib, Lq=1, H=1 << 24, Hk=1, **ws) == _attend(lib, Lq=(1 << 31) - 1, LqPad=most, H=1, Hk=1, **ws) == B.E_SHAPE
+    assert _attend(lib, Lq=most, LqPad=most, **ws) == _attend(lib, keep=(1 << 31) - 1, **ws) == B.E_SHAPE
+
+
 def test_rope_axes_table():
     freq, axis = B.chorus_rope_axes_table((16, 24), device="cpu")
     want = [10000.0 ** (-2.0 * i / 16) for i in range(8)] + [10000.0 ** (-2.0 * i / 24) for i in range(12)]

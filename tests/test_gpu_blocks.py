@@ -255,6 +255,19 @@ def test_block_mean(H, dh, L, block):
     assert (np.abs(host_bf16(out) - ref) <= U * np.abs(ref) + 2.0 ** -17 * mag).all()
 
 
+@pytest.mark.parametrize("scale", [2.0 ** 126, 2.0 ** -127, 2.0 ** -131])
+@pytest.mark.parametrize("dh,block", [(64, 128), (128, 64)])
+def test_block_mean_far_scales(dh, block, scale):
+    """Values whose sum fp32 does not hold though it holds their mean, and subnormal ones (steps of 2^-133: half a one is allowed)."""
+    print(f"[case] block_mean dh={dh} block={block} scale={scale}", flush=True)
+    L = 3 * block - 5
+    X = _bf(np.random.default_rng(block).uniform(0.25, 3.9, (2, L, dh)) * scale)
+    out = torch.empty(2, 3, dh, dtype=BF, device=DEV)
+    B.chorus_block_mean(dev_bf16(X), out, L, block)
+    ref = OB.block_mean(X, L, block)
+    assert (np.abs(host_bf16(out) - ref) <= (U + 2.0 ** -17) * np.abs(ref) + 2.0 ** -134).all()
+
+
 @pytest.mark.parametrize("H,dh,L,dims", [(4, 64, 130, (16, 24)), (12, 128, 301, (44, 42, 42)), (1, 64, 1, (64,)), (4, 128, 77, (16, 32, 32, 48)),
                                          (40, 128, 33, (96,)), (5, 64, 9, (16, 0, 16)), (7, 128, 5, ())])
 @pytest.mark.parametrize("norm", ["none", "width", "head"])
@@ -287,6 +300,13 @@ def test_rope_axes(H, dh, L, dims, norm, halves):
     assert not got[:, L:].any()
 
 
+@pytest.mark.parametrize("H", [9, 14, 18, 27, 30, 41])
+@pytest.mark.parametrize("norm,halves", [("width", False), ("width", True), ("head", False), ("head", True)])
+def test_rope_axes_widths(H, norm, halves):
+    """Rows that fill the registers they are held in partly, and one that is too wide for them."""
+    test_rope_axes(H, 128, 5, (16, 48, 32), norm, halves)
+
+
 def test_rope_axes_of_grid_positions_is_qk_norm_rope():
     """The framework's own rotation is the one of three axes with the grid's positions: same values but for the last roundings."""
     print("[case] rope_axes against qk_norm_rope", flush=True)
@@ -305,6 +325,46 @@ def test_rope_axes_of_grid_positions_is_qk_norm_rope():
 
 
 # ------------------------------------------------------------------------------------------------ together
+
+def test_attention_blocks_two_calls_at_once():
+    """Cut lists on two streams and in two captured graphs, each with a workspace of its own and kept busy for many calls: the bits of a call alone."""
+    print("[case] attention_blocks at once", flush=True)
+    rng = np.random.default_rng(21)
+    H, dh, Lq, Lk, keep = 3, 128, 200, 6400, 90
+    need = B.chorus_attention_blocks_workspace_bytes(Lq, H, dh, keep)
+    assert need > 0
+
+    def inputs():
+        Q, K, V = (_bf(rng.standard_normal((H, n, dh))) for n in (Lq, Lk, Lk))
+        return dev_bf16(Q), dev_bf16(K), _vt(V, Lk), torch.zeros(Lq, H * dh, dtype=BF, device=DEV), _i32(_lists(rng, H, Lq, Lk, keep, "gaps"))
+
+    sides = [(inputs(), torch.full((need,), 0xff, dtype=torch.uint8, device=DEV), torch.cuda.Stream()) for _ in range(2)]
+    want = []
+    for a, ws, _ in sides:
+        want.append(B.chorus_attention_blocks(*a, Lq, Lk).clone())
+        a[3].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, ws, s in sides:
+            with torch.cuda.stream(s):
+                B.chorus_attention_blocks(*a, Lq, Lk, ws=ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[3], w) for (a, _, _), w in zip(sides, want))
+    graphs = []
+    for a, ws, _ in sides:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            B.chorus_attention_blocks(*a, Lq, Lk, ws=ws)
+    for _ in range(5):
+        for a, _, _ in sides:
+            a[3].zero_()
+        torch.cuda.synchronize()
+        for g, (_, _, s) in zip(graphs, sides):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[3], w) for (a, _, _), w in zip(sides, want))
+
 
 def _pipeline(x, V0, gains, pos, freq, axis, L, H, dh, keep, bufs):
     """Projection rows -> attention output, as a caller that runs a block's operations itself calls them."""
