@@ -367,17 +367,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
     bf16x8 qf[T][KC];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const int row = first + 16 * t + l16 < nq ? first + 16 * t + l16 : nq - 1;
+      const int of = 16 * t + l16 < R ? 16 * t + l16 : R - 1, row = first + of < nq ? first + of : nq - 1;
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) qf[t][kc] = *reinterpret_cast<const bf16x8*>(q0 + (long)row * DH + 32 * kc + 8 * g);
     }
-    // strips of 16 keys, two in flight behind the one in use; behind the last strip the last again
+    // strips of 16 keys, two in flight behind the one in use; behind the last strip one key for all lanes, which costs next to nothing
     const uint32_t whole = l16 * DH + 8 * g, cut = (16 * last + l16 < nk ? l16 : nk - 1 - 16 * last) * DH + 8 * g;
     bf16x8 kf[3][KC];
     auto fetch = [&](bf16x8(&to)[KC], int strip) {
-      strip = strip < last ? strip : last;
-      const uint16_t* from = km + (long)strip * 16 * DH;
-      const uint32_t off = strip == last ? cut : whole;
+      const uint16_t* from = km + (long)(strip > last ? 0 : strip) * 16 * DH;
+      const uint32_t off = strip > last ? 0 : strip == last ? cut : whole;
 #pragma unroll
       for (int kc = 0; kc < KC; ++kc) to[kc] = *reinterpret_cast<const bf16x8*>(from + off + 32 * kc);
     };
