@@ -364,25 +364,32 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   for (int i = 0; i < (NV > 0 ? NV : 1); ++i) of_block[i] = rule_of(i);
   {
     const int l16 = lane & 15, g = lane >> 4;
+    // A lane's KC fragments are neighbouring pieces of 16 bytes of its row. Read as they stand, each lane would be a request of its own, which is
+    // what the sweep then waits for (591 x 1182 blocks, 40 heads, 91 us instead of 77; 256 x 512, 12 heads, 14.8 instead of 11.8); so KC
+    // neighbouring lanes read the pieces of one row, KC rows in turn, and exchange them.
+    const int r0 = l16 / KC * KC, piece = KC * g + l16 % KC;
     bf16x8 qf[T][KC];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const int of = 16 * t + l16 < R ? 16 * t + l16 : R - 1, row = first + of < nq ? first + of : nq - 1;
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) qf[t][kc] = *reinterpret_cast<const bf16x8*>(q0 + (long)row * DH + 32 * kc + 8 * g);
+      for (int j = 0; j < KC; ++j) {
+        const int of = 16 * t + r0 + j < R ? 16 * t + r0 + j : R - 1, row = first + of < nq ? first + of : nq - 1;
+        qf[t][j] = *reinterpret_cast<const bf16x8*>(q0 + (long)row * DH + piece * 8);
+      }
+      transpose_lanes(qf[t], lane);
     }
     // strips of 16 keys, two in flight behind the one in use; behind the last strip one key for all lanes, which costs next to nothing
-    const uint32_t whole = l16 * DH + 8 * g, cut = (16 * last + l16 < nk ? l16 : nk - 1 - 16 * last) * DH + 8 * g;
     bf16x8 kf[3][KC];
     auto fetch = [&](bf16x8(&to)[KC], int strip) {
       const uint16_t* from = km + (long)(strip > last ? 0 : strip) * 16 * DH;
-      const uint32_t off = strip > last ? 0 : strip == last ? cut : whole;
+      const int most = strip > last ? 0 : strip == last ? nk - 1 - 16 * last : 15;
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) to[kc] = *reinterpret_cast<const bf16x8*>(from + off + 32 * kc);
+      for (int j = 0; j < KC; ++j) to[j] = *reinterpret_cast<const bf16x8*>(from + (uint32_t)((r0 + j < most ? r0 + j : most) * DH + piece * 8));
     };
     uint32_t k2 = 0;  // as bits: a NaN is above all numbers, and the sign of one is dropped
     uint32_t* to = score + (long)l16 * stride + 4 * g;
-    auto use = [&](const bf16x8(&kf)[KC], int strip) {
+    auto use = [&](bf16x8(&kf)[KC], int strip) {
+      transpose_lanes(kf, lane);
       f32x4 s[T], n2 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int t = 0; t < T; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -497,7 +504,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
 // The rows of a workgroup. All of them share one sweep over a head's keys, which is what the call waits for (1182 blocks of 128 values are 300 KB, from
 // the L2, and a compute unit holds one workgroup): as few as let the launch run in one round of workgroups, and where it takes more than
 // one, 32 (two matrix tiles) or as many as their scores leave room for in the LDS, down to two rows of CHORUS_BLOCK_SELECT_MAX scores
-// (128 KB). 103 x 205 blocks, 12 heads: 8 rows 13 us, 4 rows (312 workgroups) 20.
+// (128 KB). 103 x 205 blocks, 12 heads: 8 rows 9.2 us, 4 rows (312 workgroups) half as long again.
 int select_rows(long nq, int H, int stride) {
   int R = 4;
   while (R < 32 && (nq + R - 1) / R * H > 256) R *= 2;

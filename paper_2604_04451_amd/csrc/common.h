@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "chorus.h"
 
@@ -144,6 +145,30 @@ __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, row_rotate<4>(v));
   v = fmaxf(v, row_rotate<2>(v));
   return fmaxf(v, row_rotate<1>(v));
+}
+
+// N = 2 or 4 fragments among N neighbouring lanes: the one in register j of lane b goes to register b of lane j.
+template <int N>
+__device__ __forceinline__ void transpose_lanes(bf16x8 (&x)[N], int lane) {
+  static_assert(N == 2 || N == 4, "");
+  auto swap = [](bf16x8& a, bf16x8& b, bool odd, auto ctrl) {  // lanes with the bit: the other lane's b into a; lanes without: its a into b
+    u32x4 u = __builtin_bit_cast(u32x4, a), v = __builtin_bit_cast(u32x4, b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t from_u = __builtin_amdgcn_update_dpp(0, u[k], decltype(ctrl)::value, 0xf, 0xf, true);
+      const uint32_t from_v = __builtin_amdgcn_update_dpp(0, v[k], decltype(ctrl)::value, 0xf, 0xf, true);
+      u[k] = odd ? from_v : u[k];
+      v[k] = odd ? v[k] : from_u;
+    }
+    a = __builtin_bit_cast(bf16x8, u);
+    b = __builtin_bit_cast(bf16x8, v);
+  };
+#pragma unroll
+  for (int j = 0; j < N; j += 2) swap(x[j], x[j + 1], lane & 1, std::integral_constant<int, 0xb1>{});
+  if (N == 4) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) swap(x[j], x[(j + 2) % N], lane & 2, std::integral_constant<int, 0x4e>{});
+  }
 }
 
 // Workgroup barrier that orders LDS traffic only: waits for this wave's LDS operations

@@ -6,8 +6,6 @@
 //
 // One rounding to bf16, at the end; all else in fp32. The angle is formed in fp64, in turns, and reduced to half a turn before it
 // becomes fp32: a far position (10^5 and more on one axis) keeps the phase that fp32 products would lose.
-#include <type_traits>
-
 #include "chorus_ops.h"
 #include "common.h"
 
