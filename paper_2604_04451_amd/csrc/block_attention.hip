@@ -156,9 +156,10 @@ __global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t
   bf16x8 qf[RB][KC];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    long q = (long)qb * BQ + wave * 32 + 16 * rb + lq;
+    // four neighbouring lanes read 64 bytes of a row, which is a request; what they hold is another lane's, where lq % 4 and g change places
+    long q = (long)qb * BQ + wave * 32 + 16 * rb + (lq & 12) + g;
     if (q > Lq - 1) q = Lq - 1;
-    const uint16_t* qp = Q + ((long)head * LqPad + q) * DH + 8 * g;
+    const uint16_t* qp = Q + ((long)head * LqPad + q) * DH + 8 * (lq & 3);
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
   }
@@ -240,7 +241,13 @@ __global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) asm volatile("" : "+v"(qf[rb][kc]));  // resident before the loop, which would wait for them otherwise
+    for (int kc = 0; kc < KC; ++kc) {
+      u32x4 u = __builtin_bit_cast(u32x4, qf[rb][kc]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[e] = __builtin_amdgcn_ds_bpermute(4 * (16 * (lq & 3) + (lq & 12) + g), u[e]);
+      qf[rb][kc] = __builtin_bit_cast(bf16x8, u);
+      asm volatile("" : "+v"(qf[rb][kc]));  // resident before the loop, which would wait for them otherwise
+    }
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   if (b0 >= 0) {
 #pragma unroll
@@ -324,26 +331,39 @@ __global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // no load may land in the LDS of a workgroup that has ended
   if (half == 0) asm volatile("s_barrier" ::: "memory");  // as many as the other half, where the lists are as long
 
-  const long D = (long)H * DH;
+  // On the way out, as with the queries, four neighbouring lanes write 64 bytes of a row: they get them from the lanes of that row.
+  const auto from_lane = [](int src, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)v); };
+  const int row0 = wave * 32 + (lq & 12) + g, b4 = lq & 3;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int row = wave * 32 + 16 * rb + lq;
-    const long q = (long)qb * BQ + row;
-    if (q >= Lq) continue;
+    const int row = row0 + 16 * rb;
+    const bool live = (long)qb * BQ + row < Lq;
     const float l = l_run[rb][0];
     if (sliced) {
-      const long at = (long)(unit - whole) * BQ + row;
-      float* op = part + at * DH + 4 * g;
+      const long at = (long)(unit - whole) * BQ;
+      float* op = part + (at + row) * DH + 4 * b4;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(op + 16 * db) = o[db][rb];
-      if (g == 0) reinterpret_cast<float2*>(part + (long)(units - whole) * BQ * DH)[at] = make_float2(m_run[rb], l);
+      for (int db = 0; db < DB; ++db) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(from_lane(16 * b4 + (lq & 12) + g, __float_as_uint(o[db][rb][e])));
+        if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
+      }
+      if (g == 0 && (long)qb * BQ + wave * 32 + 16 * rb + lq < Lq)
+        reinterpret_cast<float2*>(part + (long)(units - whole) * BQ * DH)[at + wave * 32 + 16 * rb + lq] = make_float2(m_run[rb], l);
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
-      uint16_t* op = O + q * D + (long)head * DH + 4 * g;
+      uint16_t* op = O + ((long)qb * BQ + row) * ((long)H * DH) + (long)head * DH + 8 * b4;
+      const int src = 16 * (b4 >> 1 | (b4 & 1) << 1) + (lq & 12) + g;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        *reinterpret_cast<uint2*>(op + 16 * db) = make_uint2(pack_bf16x2(o[db][rb][0] * inv, o[db][rb][1] * inv),
-                                                             pack_bf16x2(o[db][rb][2] * inv, o[db][rb][3] * inv));
+      for (int i = 0; i < DB / 2; ++i) {
+        // 4 values of block 2i and 4 of 2i + 1 here, and as many with the lane 16 further: after the swap eight of the one here, of the other there
+        const f32x4 x = o[2 * i][rb] * inv, y = o[2 * i + 1][rb] * inv;
+        const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[0], x[1]), pack_bf16x2(y[0], y[1]), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[2], x[3]), pack_bf16x2(y[2], y[3]), false, false);
+        const u32x4 v = {from_lane(src, lo[0]), from_lane(src, hi[0]), from_lane(src, lo[1]), from_lane(src, hi[1])};
+        if (live) *reinterpret_cast<u32x4*>(op + 32 * i) = v;
+      }
     }
   }
 #endif
