@@ -8,8 +8,9 @@
 //
 // What a step has to fit into: 68 MFMAs a wave (1088 cycles of the pipe), 32 exponentials (512) and about 90 other vector instructions.
 // Measured (cycles a step, 32760 queries, 103 blocks each, 12 heads): vector phase 1240, matrix phase 1435, so the matrix pipe is busy
-// three quarters of the time at the clock that the power management leaves; 1310 TFLOP/s, where the dense kernel has 1380 over 13184
-// keys and 1170 over as many as these lists hold. On the way there: two workgroups of four waves with the next logits made beside the
+// three quarters of the time at the clock that the power management leaves; 1030 us, 1290 TFLOP/s, where the dense kernel has 1380 over 13184
+// keys and 1170 over as many as these lists hold (all three a few percent apart from card to card). The probabilities are rounded to bf16 for
+// the matrix pipe, once, and their sum is taken over the rounded ones. On the way there: two workgroups of four waves with the next logits made beside the
 // exponentials of this tile 1165 (the two pipes hardly overlap inside a wave); loops that were unrolled by two for constant buffer
 // addresses 1060 (the register allocator gives every MFMA result a new home then, and reads wait for the old ones).
 //

@@ -75,10 +75,10 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
 // that are flushed. Norms come from the same pipe (the diagonal of K K^T) and are within 2^-16 of their values, which kBound has room for.
 // Where |q| |k| is a number below 1e38 every score is one; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
 //
-// Half of a workgroup's time goes into the sweep over the keys, half into its rows; there the vector and the scalar pipe share the work, 20
-// comparisons and 40 counts for each look at the scores of 1182 blocks. The search therefore stays in floats, with no more than a mean
-// between two looks (compared and bisected as integers, for a sure end: 114 us and 21.5 instead of 92 and 17): a block that is in whatever its score
-// (`always`) scores +inf, one that is out -inf.
+// Two fifths of a workgroup's time go into the sweep over the keys (20K of 48K cycles at 591 x 1182 blocks, 40 heads: 77 us), the rest into its
+// rows; there the vector and the scalar pipe share the work, 20 comparisons and 40 counts for each look at a row. The search therefore stays
+// in floats, with no more than a mean between two looks (compared and bisected as integers, for a sure end, it took a quarter longer): a block
+// that is in whatever its score (`always`) scores +inf, one that is out -inf.
 // ---------------------------------------------------------------------------
 constexpr uint32_t kIn = 0xffffffffu, kOut = 0u;  // the same two as codes: no finite float has them
 constexpr float kBound = 1.05f / 65536.0f;
