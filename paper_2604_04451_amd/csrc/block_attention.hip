@@ -1,16 +1,18 @@
 // Attention over listed blocks of keys: O = softmax(Q K^T / sqrt(dh)) V, a query seeing the keys of the blocks in the list of its block of
 // 128 queries and head, and no others. bf16 operands on the matrix pipe, fp32 online softmax, logits never leave registers.
 //
-// A workgroup of eight waves takes two lists, each half of it one: a wave holds 32 of the 128 queries (two blocks of 16, in registers) and
-// its half walks over the list a block of 64 keys at a time, in tiles of its own in LDS. The halves are half a step apart: while the
-// waves of one make the weights of a tile on the vector pipe, those of the other keep the matrix pipe busy (O += V P, then the next tile's
-// S = K Q^T), one wave of each on every SIMD. Neighbouring lists meet many of the same blocks, which then come from the L2.
+// A workgroup of four waves takes a list: a wave holds 32 of the 128 queries (two blocks of 16, in registers) and all walk over the list a
+// block of 64 keys at a time, in tiles in LDS. A compute unit holds two workgroups, a wave of each on every SIMD. They get half a step apart by
+// themselves, the matrix phase going ahead of the other's vector phase: while the waves of one make the weights of a tile on the vector pipe, those
+// of the other keep the matrix pipe busy (O += V P, then the next tile's S = K Q^T). Held apart by barriers across both, as one workgroup with
+// two lists, they are no faster where lists are alike (32760 queries 1026 us, 1014 as they are) and wait for each other where they are not
+// (13104 queries with 30 to 60 blocks, 12 heads: 236 us, 215). Neighbouring lists meet many of the same blocks, which then come from the L2.
 //
 // What a step has to fit into: 68 MFMAs a wave (1088 cycles of the pipe), 32 exponentials (512) and about 90 other vector instructions.
 // Measured (cycles a step, 32760 queries, 103 blocks each, 12 heads): vector phase 1240, matrix phase 1435, so the matrix pipe is busy
-// three quarters of the time at the clock that the power management leaves; 1030 us, 1290 TFLOP/s, where the dense kernel has 1380 over 13184
+// three quarters of the time at the clock that the power management leaves; 1014 us, 1310 TFLOP/s, where the dense kernel has 1380 over 13184
 // keys and 1170 over as many as these lists hold (all three a few percent apart from card to card). The probabilities are rounded to bf16 for
-// the matrix pipe, once, and their sum is taken over the rounded ones. On the way there: two workgroups of four waves with the next logits made beside the
+// the matrix pipe, once, and their sum is taken over the rounded ones. On the way there: the next logits made beside the
 // exponentials of this tile 1165 (the two pipes hardly overlap inside a wave); loops that were unrolled by two for constant buffer
 // addresses 1060 (the register allocator gives every MFMA result a new home then, and reads wait for the old ones).
 //
@@ -29,20 +31,20 @@ constexpr int64_t kMostKeys = 1 << 22;  // a head's keys and values in bytes sta
 constexpr int kMostSlices = 64;         // the join holds a slice a lane
 constexpr int64_t kMostLists = (1 << 24) - 512 * kMostSlices - 2;  // with the last round's slices, 256 threads each, within the 2^32 of a launch
 
-// How a launch goes: the first `whole` lists by one half of a workgroup each, the others cut into `slices` (entry e of a list goes to slice
+// How a launch goes: the first `whole` lists by one workgroup each, the others cut into `slices` (entry e of a list goes to slice
 // e % slices, so that a short list with its end full of -1 is cut evenly), whose results are joined by a second launch.
 struct BlockPlan {
   long whole;
   int cut, slices;
 };
-// Lists that leave the last round of half workgroups partly empty (or the only one) are cut into as many slices as make that round the shortest:
-// a half takes about 1.6 us a block; a slice costs its fp32 result on the way out and in (4 TB/s), the join a launch.
+// Lists that leave the last round of workgroups (two on a compute unit) partly empty, or the only one, are cut into as many slices as make that
+// round the shortest: a workgroup takes about 1.6 us a block; a slice costs its fp32 result on the way out and in (4 TB/s), the join a launch.
 BlockPlan block_plan(long lists, int dh, int keep) {
-  constexpr long halves = 2 * 256;
-  const long cut = lists % halves;
+  constexpr long places = 2 * 256;
+  const long cut = lists % places;
   BlockPlan best{lists, 0, 1};
   auto cost = [&](long s) {
-    const long rounds = (cut * s + halves - 1) / halves;
+    const long rounds = (cut * s + places - 1) / places;
     return 1.6 * (double)rounds * (double)((keep + s - 1) / s) + (s > 1 ? 6.0 + (double)(cut * s) * BQ * dh * 8.0 / 4e6 : 0.0);
   };
   double least = cost(1);
@@ -80,28 +82,24 @@ struct List {
 
 // PRE: the queries hold log2(e) / sqrt(dh) already, and a logit leaves the matrix pipe as the exponent of its weight.
 template <int DH, bool PRE>
-__global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K,
+__global__ __launch_bounds__(256, 2) void attention_blocks_kernel(const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K,
                                                                   const uint16_t* __restrict__ Vt, uint16_t* __restrict__ O,
                                                                   const int* __restrict__ blocks, float* __restrict__ part, long Lq,
                                                                   long Lk, long LqPad, long LkPad, int H, int group, int nq, int nk, int keep,
-                                                                  int whole, int slices, int units, int pairs, float scale_log2) {
+                                                                  int whole, int slices, float scale_log2) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the buffer descriptors below are types of the device compiler's alone
   constexpr int KB = BK / 16, NC = BK / 32, KC = DH / 32, DB = DH / 16, RB = 2;
   constexpr int K_LD = DH / 32, V_LD = DH / 32;  // 1 KB loads of a wave for a tile
   constexpr int TILE = BK * DH;                  // elements of a tile of keys or values
-  extern __shared__ __attribute__((aligned(16))) uint16_t smem_all[];  // for each half of the workgroup: [2][TILE] keys, [2][TILE] values
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values
   typedef __attribute__((address_space(3))) void* Lds;
 
   const int tid = threadIdx.x, lane = tid & 63;
-  const int half = __builtin_amdgcn_readfirstlane(tid >> 8), wave = __builtin_amdgcn_readfirstlane(tid >> 6 & 3);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
-  uint16_t* const smem = smem_all + half * 4 * TILE;
-  // a wave that ends is not waited for at a barrier: neither a half without a list nor one with the shorter list holds up the other
-  // (cut lists come last, in ranges of their own on every XCD: with the others' they would all be on the last one)
-  const int front = whole < units && pairs ? whole / 2 : 0;
-  const int wg = (int)blockIdx.x < front ? xcd_remap(blockIdx.x, front) : front + xcd_remap(blockIdx.x - front, gridDim.x - front);
-  const int unit = pairs ? 2 * wg + half : half ? units : wg;
-  if (unit >= units) return;
+  // cut lists come last, in ranges of their own on every XCD: with the others' they would all be on the last one
+  const int units = gridDim.x, front = whole < units ? whole : 0;
+  const int unit = (int)blockIdx.x < front ? xcd_remap(blockIdx.x, front) : front + xcd_remap(blockIdx.x - front, units - front);
   const bool sliced = unit >= whole;
   const int tile = sliced ? whole + (unit - whole) / slices : unit, slice = sliced ? (unit - whole) % slices : 0;
   const int head = tile / nq, qb = tile - head * nq;
@@ -261,7 +259,6 @@ __global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t
       }
   }
   asm volatile("s_barrier" ::: "memory");
-  if (half == 1) asm volatile("s_barrier" ::: "memory");  // run one phase behind the other half
 
   for (int buf = 0; b0 >= 0; buf ^= 1) {
     // ================= vector phase: the weights of this tile =================
@@ -329,8 +326,7 @@ __global__ __launch_bounds__(512, 2) void attention_blocks_kernel(const uint16_t
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // no load may land in the LDS of a workgroup that has ended
-  if (half == 0) asm volatile("s_barrier" ::: "memory");  // as many as the other half, where the lists are as long
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may land in the LDS of a workgroup that has ended
 
   // On the way out, as with the queries, four neighbouring lanes write 64 bytes of a row: they get them from the lanes of that row.
   const auto from_lane = [](int src, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)v); };
@@ -452,17 +448,15 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
   const size_t need = plan_bytes(p, dh);
   if (need && (!ws || ws_bytes < need)) return CHORUS_E_WORKSPACE;
   const float scale_log2 = prescaled ? 1.0f : CHORUS_ATTENTION_Q_PRESCALE(dh);
-  const long units = p.whole + (long)p.cut * p.slices;
-  const int pairs = units > 256;  // fewer lists than compute units: one each
-  const dim3 grid((unsigned)(pairs ? (units + 1) / 2 : units));
+  const dim3 grid((unsigned)(p.whole + (long)p.cut * p.slices));
 #define ATTEND(DH, PRE)                                                                                                                 \
   do {                                                                                                                                  \
     static DynLdsOnce once;                                                                                                             \
-    constexpr int lds = 8 * BK * DH * 2;                                                                                                \
+    constexpr int lds = 4 * BK * DH * 2;                                                                                                \
     CHK_STATUS(once.ensure((const void*)attention_blocks_kernel<DH, PRE>, lds));                                                        \
-    hipLaunchKernelGGL((attention_blocks_kernel<DH, PRE>), grid, dim3(512), lds, (hipStream_t)stream, Q, K, Vt, O, blocks, (float*)ws,   \
-                       (long)Lq, (long)Lk, (long)LqPad, (long)LkPad, H, H / Hk, (int)nq, (int)nk, keep, (int)p.whole, p.slices, (int)units, \
-                       pairs, scale_log2);                                                                                              \
+    hipLaunchKernelGGL((attention_blocks_kernel<DH, PRE>), grid, dim3(256), lds, (hipStream_t)stream, Q, K, Vt, O, blocks, (float*)ws,   \
+                       (long)Lq, (long)Lk, (long)LqPad, (long)LkPad, H, H / Hk, (int)nq, (int)nk, keep, (int)p.whole, p.slices, \
+                       scale_log2);                                                                                                     \
   } while (0)
   if (dh == 128) {
     if (prescaled) ATTEND(128, true);
