@@ -38,18 +38,22 @@ struct BlockPlan {
   int cut, slices;
 };
 // Lists that leave the last round of workgroups (two on a compute unit) partly empty, or the only one, are cut into as many slices as make that
-// round the shortest: a workgroup takes about 1.6 us a block; a slice costs its fp32 result on the way out and in (4 TB/s), the join a launch.
+// round the shortest. A block takes a workgroup of heads of 128 about 1.2 us alone on its unit and 1.5 beside another, heads of 64 seven tenths of
+// that; a slice costs its fp32 result on the way out and in (3 TB/s), the join 8 us. us, lists of blocks, dh: 40 of 118, 128: 6 slices 36, 1 124, 12
+// 40; 32 of 30, 64: 6 slices 15, 1 26, 16 20; 256 of 100, 128: 2 slices 97, 1 122, 4 107; 312 of 20, 128: whole 36, 2 slices 49.
 BlockPlan block_plan(long lists, int dh, int keep) {
-  constexpr long places = 2 * 256;
+  constexpr long units = 256, places = 2 * units;
   const long cut = lists % places;
   BlockPlan best{lists, 0, 1};
   auto cost = [&](long s) {
-    const long rounds = (cut * s + places - 1) / places;
-    return 1.6 * (double)rounds * (double)((keep + s - 1) / s) + (s > 1 ? 6.0 + (double)(cut * s) * BQ * dh * 8.0 / 4e6 : 0.0);
+    const long n = cut * s, rounds = n / places, rest = n % places;
+    const double last = rest == 0 ? 0.0 : rest <= units && n == rest && lists < places ? 1.2 : 1.5;
+    return (1.5 * (double)rounds + last) * (dh == 128 ? 1.0 : 0.7) * (double)((keep + s - 1) / s) +
+           (s > 1 ? 8.0 + (double)n * BQ * dh * 8.0 / 3e6 : 0.0);
   };
   double least = cost(1);
   for (int s = 2; cut > 0 && s <= kMostSlices && s <= keep; ++s)
-    if (cost(s) < 0.95 * least) {
+    if (cost(s) < 0.9 * least) {
       least = cost(s);
       best = BlockPlan{lists - cut, (int)cut, s};
     }
