@@ -743,11 +743,12 @@ def chorus_rope_axes(inp, col0, gain, norm, out, L, H, dh, pos, freq, axis, layo
     _chk(pos, torch.float32, "pos")
     _chk(freq, torch.float64, "freq")
     _chk(axis, torch.int32, "axis", freq.shape)
-    ld, Lpad = inp.shape[1], out.shape[1]
-    if tuple(out.shape) != (H, Lpad, dh) or col0 < 0 or col0 + H * dh > ld or inp.shape[0] < L or pos.dim() != 2 or pos.shape[0] < L:
+    rows, to, at = inp.shape, out.shape, pos.shape
+    ld, Lpad = rows[1], to[1]
+    if to != (H, Lpad, dh) or col0 < 0 or col0 + H * dh > ld or rows[0] < L or len(at) != 2 or at[0] < L:
         raise TypeError("shape mismatch")
     _status("chorus_rope_axes", lib.chorus_rope_axes(inp.data_ptr() + 2 * col0, ld, _p(gain), int(norm), _p(out), L, Lpad, H, dh, _p(pos),
-                                                     pos.shape[1], _p(freq), _p(axis), freq.numel(), int(layout), float(out_scale),
+                                                     at[1], _p(freq), _p(axis), freq.numel(), int(layout), float(out_scale),
                                                      _stream()))
     return out
 
@@ -790,11 +791,12 @@ def chorus_attention_blocks(Q, K, Vt, O, blocks, Lq, Lk, prescaled=False, ws=Non
     _chk(blocks, torch.int32, "blocks")
     H, LqPad, dh = Q.shape
     Hk, LkPad, _ = K.shape
-    if K.shape[2] != dh or tuple(Vt.shape) != (Hk * dh, LkPad) or O.shape[1] != H * dh or O.shape[0] < Lq:
+    out, lists = O.shape, blocks.shape
+    if K.shape[2] != dh or Vt.shape != (Hk * dh, LkPad) or out[1] != H * dh or out[0] < Lq:
         raise TypeError("shape mismatch")
-    if blocks.dim() != 3 or tuple(blocks.shape[:2]) != (H, -(-Lq // BLOCK_QUERIES)):
+    if len(lists) != 3 or lists[0] != H or lists[1] != -(-Lq // BLOCK_QUERIES):
         raise TypeError("blocks: wrong shape")
-    keep = blocks.shape[2]
+    keep = lists[2]
     _chk(ws, torch.uint8, "ws")
     if ws is None:
         need = lib.chorus_attention_blocks_workspace_bytes(Lq, H, dh, keep)
