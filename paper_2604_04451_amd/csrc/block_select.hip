@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
 //
 // How far a score can be off: products of bf16 are exact in fp32, and whatever the order of a sum of DH <= 128 of them, each of its
 // additions is off by at most 2^-23 of the sum of magnitudes, itself at most |q| |k|: kBound |q| max |k|, and a trace for values
-// that are flushed. Norms come from the same pipe (the diagonal of K K^T) and are within 2^-16 of their values, which kBound has room for.
+// that are flushed. Norms come from the same pipe (the largest entry of K K^T, which is on its diagonal) and are within 2^-16 of their values, which kBound has room for.
 // Where |q| |k| is a number below 1e38 every score is one; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
 //
 // Two fifths of a workgroup's time go into the sweep over the keys (20K of 48K cycles at 591 x 1182 blocks, 40 heads: 77 us), the rest into its
@@ -379,12 +379,18 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
       transpose_lanes(qf[t], lane);
     }
     // strips of 16 keys, two in flight behind the one in use; behind the last strip one key for all lanes, which costs next to nothing
+    const uint32_t whole = (r0 * DH + piece * 8) * 2;
     bf16x8 kf[3][KC];
     auto fetch = [&](bf16x8(&to)[KC], int strip) {
-      const uint16_t* from = km + (long)(strip > last ? 0 : strip) * 16 * DH;
-      const int most = strip > last ? 0 : strip == last ? nk - 1 - 16 * last : 15;
+      const char* from = reinterpret_cast<const char*>(km + (long)(strip > last ? 0 : strip) * 16 * DH);
+      if (KC == 4 && strip < last) {  // one address for four loads; two are not worth the branch
 #pragma unroll
-      for (int j = 0; j < KC; ++j) to[j] = *reinterpret_cast<const bf16x8*>(from + (uint32_t)((r0 + j < most ? r0 + j : most) * DH + piece * 8));
+        for (int j = 0; j < KC; ++j) to[j] = *reinterpret_cast<const bf16x8*>(from + whole + j * DH * 2);
+      } else {
+        const int most = strip > last ? 0 : strip == last ? nk - 1 - 16 * last : 15;
+#pragma unroll
+        for (int j = 0; j < KC; ++j) to[j] = *reinterpret_cast<const bf16x8*>(from + (uint32_t)((r0 + j < most ? r0 + j : most) * DH + piece * 8) * 2);
+      }
     };
     uint32_t k2 = 0;  // as bits: a NaN is above all numbers, and the sign of one is dropped
     uint32_t* to = score + (long)l16 * stride + 4 * g;
@@ -399,10 +405,11 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
         for (int t = 0; t < T; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kc], qf[t][kc], s[t], 0, 0, 0);
         n2 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kc], kf[kc], n2, 0, 0, 0);
       }
-      // the diagonal is with the lanes g = l16 / 4, in element l16 % 4
-      const float d = l16 & 2 ? (l16 & 1 ? n2[3] : n2[2]) : (l16 & 1 ? n2[1] : n2[0]);
-      const uint32_t bits = __float_as_uint(d) & 0x7fffffffu;
-      k2 = bits > k2 ? bits : k2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t bits = __float_as_uint(n2[i]) & 0x7fffffffu;
+        k2 = bits > k2 ? bits : k2;
+      }
 #pragma unroll
       for (int t = 0; t < T; ++t)
         if (T > 1 || l16 < R) *reinterpret_cast<u32x4*>(to + (long)t * 16 * stride + strip * 16) = __builtin_bit_cast(u32x4, s[t]);
@@ -423,7 +430,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
       fetch(kf[1], strip + 4 * WAVES);
       use(kf[2], strip + 2 * WAVES);
     }
-    k2 = wave_max_u32(g == l16 >> 2 ? k2 : 0);
+    k2 = wave_max_u32(k2);
     if (lane == 0) s_k2[wave] = k2;
     if (wave == 0) {
 #pragma unroll
