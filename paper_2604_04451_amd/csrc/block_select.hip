@@ -574,7 +574,7 @@ int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_
     if (R == 32) SELECT(DH, NV, 2, THREADS);   \
     else SELECT(DH, NV, 1, THREADS);           \
   } while (0)
-  // A row's scores stay in registers up to 40 a lane; behind that they are read from LDS at each look (2 rows of 9000 blocks: 145 us).
+  // A row's scores stay in registers up to 40 a lane; behind that they are read from LDS at each look (2 rows of 9000 blocks: 109 us).
 #define SELECT_LENGTH(DH)                           \
   do {                                              \
     if (nk <= 64 * 8) SELECT_ROWS(DH, 8, 1024);     \
