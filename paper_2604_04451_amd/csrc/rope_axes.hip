@@ -99,56 +99,78 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     rstd = rsqrtf(wave_sum(ss) / (float)(H * dh) + kEps) * out_scale;
   }
   const int iters = NCH > 0 ? NCH : (nchunk + 63) / 64;
+  const int d0 = lane % lanes * 8;  // in its head, whatever the chunk
+  // Halves: a value's other half is in a lane of the same head, `off` values further. Gains go in ahead of the rotation and the norm behind it, where
+  // a value takes it once (75600 x 5120, norm of the head 300 us, both halves normalised ahead 330; norm of the row 302 and 337).
+  const bool first = d0 < n_pairs;
+  const int off = !HALVES || d0 >= 2 * n_pairs ? 0 : first ? n_pairs : -n_pairs;
+  float cs[8], sn[8];
+  if (HALVES) {
+    const int p = first ? d0 : d0 - n_pairs;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      cs[e] = off != 0 ? s_cos[wave][p + e] : 1.0f;
+      sn[e] = off == 0 ? 0.f : first ? -s_sin[wave][p + e] : s_sin[wave][p + e];
+    }
+  }
 #pragma unroll
   for (int it = 0; it < iters; ++it) {
     const int c0 = 64 * it;
     const bool live = it < FULL || c0 + lane < nchunk;
     const int c = live ? c0 + lane : nchunk - 1;  // lanes past the end keep the head's sum company and store nothing
-    const int head = c / lanes, d0 = c % lanes * 8;
-    float x[8], y[8] = {};
+    const int head = c / lanes;
+    float x[8];
     u32x4 u;
     if (NCH > 0) u = rv[NCH > 0 ? it : 0];
     else u = *reinterpret_cast<const u32x4*>(r + c * 8);
     unpack8(x, u);
     if (NORM == CHORUS_ROPE_NORM_HEAD) rstd = rsqrtf(head_sum(sum_squares(x), lanes) / (float)dh + kEps) * out_scale;
     const float* g = NORM == CHORUS_ROPE_NORM_HEAD ? gain + d0 : gain + c * 8;
-    auto scaled = [&](float(&v)[8], int off) {
-      if (NORM == CHORUS_ROPE_NORM_NONE) {
+    auto gains = [&](float(&v)[8], int at) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= rstd;
-      } else {
-        const f32x4 g0 = *reinterpret_cast<const f32x4*>(g + off), g1 = *reinterpret_cast<const f32x4*>(g + off + 4);
+      for (int e = 0; e < 8; e += 4) {
+        const f32x4 q = NORM == CHORUS_ROPE_NORM_NONE ? f32x4{1.f, 1.f, 1.f, 1.f} : *reinterpret_cast<const f32x4*>(g + at + e);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] *= rstd * g0[e];
-          v[4 + e] *= rstd * g1[e];
-        }
+        for (int i = 0; i < 4; ++i) v[e + i] = q[i];
       }
     };
-    scaled(x, 0);
+    float own[8];
+    gains(own, 0);
     if (HALVES) {
-      const bool first = d0 < n_pairs;
-      const int off = d0 >= 2 * n_pairs ? 0 : first ? n_pairs : -n_pairs;  // where the other half of the pairs is: in a lane of the same head
-      u32x4 other;
+      float y[8];
+      if (NORM == CHORUS_ROPE_NORM_WIDTH) {  // gains that change from chunk to chunk: exchanged with them, each is loaded once
 #pragma unroll
-      for (int k = 0; k < 4; ++k) other[k] = __shfl(u[k], lane + off / 8, 64);
-      if (off != 0) {
-        const int p = first ? d0 : d0 - n_pairs;
+        for (int e = 0; e < 8; ++e) x[e] *= own[e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], lane + off / 8, 64) * sn[e];
+      } else {
+        u32x4 other;
+        float of[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) other[k] = __shfl(u[k], lane + off / 8, 64);
         unpack8(y, other);
-        scaled(y, off);
+        gains(of, off);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float cs = s_cos[wave][p + e], sn = s_sin[wave][p + e];
-          x[e] = first ? x[e] * cs - y[e] * sn : y[e] * sn + x[e] * cs;
+          x[e] *= own[e];
+          y[e] *= of[e] * sn[e];
         }
       }
+      if (off != 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], cs[e], y[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= rstd;
     } else {
 #pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= rstd * own[e];
+#pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float cs = s_cos[wave][(d0 >> 1) + k], sn = s_sin[wave][(d0 >> 1) + k];
+        const float c_ = s_cos[wave][(d0 >> 1) + k], s_ = s_sin[wave][(d0 >> 1) + k];
         const float a = x[2 * k], b = x[2 * k + 1];
-        x[2 * k] = a * cs - b * sn;
-        x[2 * k + 1] = a * sn + b * cs;
+        x[2 * k] = a * c_ - b * s_;
+        x[2 * k + 1] = a * s_ + b * c_;
       }
     }
     u32x4 o;
