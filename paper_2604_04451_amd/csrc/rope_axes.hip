@@ -67,14 +67,14 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
       rv[i] = *reinterpret_cast<const u32x4*>(r + (i < FULL || c < nchunk ? c : nchunk - 1) * 8);
     }
   }
+  uint64_t turning;  // the pairs that do; what stands beside a value in another pair, infinities and NaN too, is kept out of it
   {
-    float cs = 1.f, sn = 0.f;  // pairs beyond the rotated ones, or of no axis
-    if (lane < n_pairs) {
-      const int a = axis[lane];
-      if ((unsigned)a < (unsigned)n_axes) {
-        const double turns = (double)pos[row * n_axes + a] * freq[lane] * 0.15915494309189535;  // / 2 pi
-        sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &sn, &cs);
-      }
+    float cs = 1.f, sn = 0.f;
+    const int a = lane < n_pairs ? axis[lane] : -1;
+    turning = __ballot((unsigned)a < (unsigned)n_axes);
+    if ((unsigned)a < (unsigned)n_axes) {
+      const double turns = (double)pos[row * n_axes + a] * freq[lane] * 0.15915494309189535;  // / 2 pi
+      sincospif(2.0f * (float)(turns - __builtin_rint(turns)), &sn, &cs);
     }
     s_cos[wave][lane] = cs;
     s_sin[wave][lane] = sn;
@@ -104,6 +104,7 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
   // a value takes it once (75600 x 5120, norm of the head 300 us, both halves normalised ahead 330; norm of the row 302 and 337).
   const bool first = d0 < n_pairs;
   const int off = !HALVES || d0 >= 2 * n_pairs ? 0 : first ? n_pairs : -n_pairs;
+  const uint32_t turns = HALVES ? (off != 0 ? (uint32_t)(turning >> (first ? d0 : d0 - n_pairs)) : 0u) : (uint32_t)(turning >> (d0 >> 1));
   float cs[8], sn[8];
   if (HALVES) {
     const int p = first ? d0 : d0 - n_pairs;
@@ -156,10 +157,8 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
           y[e] *= of[e] * sn[e];
         }
       }
-      if (off != 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_fmaf(x[e], cs[e], y[e]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = turns >> e & 1 ? __builtin_fmaf(x[e], cs[e], y[e]) : x[e];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= rstd;
     } else {
@@ -169,8 +168,8 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
       for (int k = 0; k < 4; ++k) {
         const float c_ = s_cos[wave][(d0 >> 1) + k], s_ = s_sin[wave][(d0 >> 1) + k];
         const float a = x[2 * k], b = x[2 * k + 1];
-        x[2 * k] = a * c_ - b * s_;
-        x[2 * k + 1] = a * s_ + b * c_;
+        x[2 * k] = turns >> k & 1 ? a * c_ - b * s_ : a;
+        x[2 * k + 1] = turns >> k & 1 ? a * s_ + b * c_ : b;
       }
     }
     u32x4 o;
