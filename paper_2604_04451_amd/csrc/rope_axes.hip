@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     s_sin[wave][lane] = sn;
     __builtin_amdgcn_wave_barrier();
   }
-  float rstd = out_scale;
+  float rstd = 1.0f;  // with out_scale in it; where there is no norm, out_scale is the gain: ahead of the rotation, which may leave fp32 without it
   if (NORM == CHORUS_ROPE_NORM_WIDTH) {
     float ss = 0.f, x[8];
     if (NCH > 0) {
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     auto gains = [&](float(&v)[8], int at) {
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
-        const f32x4 q = NORM == CHORUS_ROPE_NORM_NONE ? f32x4{1.f, 1.f, 1.f, 1.f} : *reinterpret_cast<const f32x4*>(g + at + e);
+        const f32x4 q = NORM == CHORUS_ROPE_NORM_NONE ? f32x4{out_scale, out_scale, out_scale, out_scale} : *reinterpret_cast<const f32x4*>(g + at + e);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[e + i] = q[i];
       }

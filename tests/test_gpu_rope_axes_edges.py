@@ -58,3 +58,19 @@ def test_no_rows_but_padding(H, L, pad):
     print(f"[case] rope_axes H={H} L=0 with {pad} rows of padding", flush=True)
     out = _rotate(np.zeros((0, H * 64), np.float32), H, 64, np.zeros((0, 2), np.float32), np.ones(32), np.zeros(32, np.int32), False, 1.0, pad)
     assert not out.view(torch.int16).any()
+
+
+@pytest.mark.parametrize("H,dh", [(3, 64), (12, 128), (41, 128)])
+@pytest.mark.parametrize("halves", [False, True])
+def test_largest_values_scaled_down(H, dh, halves):
+    """Pairs whose turned values fp32 does not hold until they are multiplied by out_scale, which the results hold again."""
+    print(f"[case] rope_axes largest H={H} dh={dh} halves={halves}", flush=True)
+    rng = np.random.default_rng(dh)
+    L = 50
+    pos = rng.uniform(-50, 50, (L, 2)).astype(np.float32)
+    freq, axis = (t.numpy() for t in B.chorus_rope_axes_table((16, 32), device="cpu"))
+    x = synth.round_bf16((rng.choice([-1.0, 1.0], (L, H * dh)) * rng.uniform(1.5, 1.9, (L, H * dh)) * 2.0 ** 127).astype(np.float32))
+    got = host_bf16(_rotate(x, H, dh, pos, freq, axis, halves, 0.25))[:, :L]
+    ref = OB.rope_axes(x, None, "none", H, dh, pos, freq, axis, halves, 0.25)
+    assert np.abs(ref).max() > 2.0 ** 126  # turned values beyond 2^128
+    assert (np.abs(got - ref) <= U * np.abs(ref) + 2.0 ** -19 * np.abs(ref).max(2, keepdims=True)).all()
