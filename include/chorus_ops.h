@@ -183,8 +183,10 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
  *   ceil(L / block); a short last block is the mean of its own rows. block: CHORUS_BLOCK_QUERIES or CHORUS_BLOCK_KEYS.
  *
  * chorus_block_select: for each of H heads and nq rows of Qm the `keep` of nk rows of Km that come first by class, score, index:
- *   Qm dev bf16 [H, nq, dh], Km dev bf16 [Hk, nk, dh] (H % Hk == 0; head h reads h / (H / Hk)); score = Qm . Km, exact products added in
- *   fp64, NaN below every number, the higher first, equal ones by ascending index
+ *   Qm dev bf16 [H, nq, dh], Km dev bf16 [Hk, nk, dh] (H % Hk == 0; head h reads h / (H / Hk)); score = Qm . Km, NaN below every
+ *   number, the higher first, equal ones by ascending index. Products are exact and added in fp64, which is exact too unless terms are
+ *   more than 2^30 apart; then the sum is that of eight consecutive values one after the other, these sums dh/16 places apart, then
+ *   dh/32, ..., 1
  *   rule   dev uint8 [nk] or NULL: 1 = ahead of all others, 2 = never, anything else by its score
  *   blocks dev int32 [H, nq, keep]: ascending, -1 behind the last
  *   nk from 1 to CHORUS_BLOCK_SELECT_MAX, nq * H at most 2^22 - 1 (CHORUS_E_SHAPE), keep >= 1.

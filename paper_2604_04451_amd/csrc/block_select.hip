@@ -106,20 +106,34 @@ __device__ __forceinline__ int lanes_below(uint64_t mask, int more) {  // of the
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, more));
 }
 
-// The score of a row of queries and a block of keys in fp64: exact, unless terms are 2^30 apart.
+// Eight products, each exact in fp64, added one after the other.
+__device__ __forceinline__ double dot8(const u32x4& x, const u32x4& y) {
+  double s = 0.0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s = __builtin_fma((double)__uint_as_float(x[e] << 16), (double)__uint_as_float(y[e] << 16), s);
+    s = __builtin_fma((double)__uint_as_float(x[e] & 0xffff0000u), (double)__uint_as_float(y[e] & 0xffff0000u), s);
+  }
+  return s;
+}
+
+// The score of a row of queries and a block of keys in fp64: exact, unless terms are 2^30 apart. Beyond that the order of
+// the additions decides, and it is close_border's, so that a row's choice is the same by either: eight values one after the
+// other, then sums that are half of them apart, a quarter, ... and neighbours.
 template <int DH>
 __device__ __forceinline__ uint64_t exact_score(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k) {
-  double s[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 4
-  for (int d = 0; d < DH; d += 8) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(q + d), b = *reinterpret_cast<const u32x4*>(k + d);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s[e] = __builtin_fma((double)__uint_as_float(a[e] << 16), (double)__uint_as_float(b[e] << 16), s[e]);
-      s[e] = __builtin_fma((double)__uint_as_float(a[e] & 0xffff0000u), (double)__uint_as_float(b[e] & 0xffff0000u), s[e]);
-    }
+  constexpr int LANES = DH / 8;
+  auto piece = [&](int l) { return dot8(*reinterpret_cast<const u32x4*>(q + 8 * l), *reinterpret_cast<const u32x4*>(k + 8 * l)); };
+  double pair = 0.0, sum = 0.0;
+#pragma unroll 1  // the sums 0, 2, 1, 3 of four, with few of the pieces in registers
+  for (int i = 0; i < 4; ++i) {
+    const int l = i >> 1 | (i & 1) << 1;
+    double s = piece(l) + piece(l + LANES / 2);
+    if (LANES == 16) s += piece(l + 4) + piece(l + 12);
+    pair = i & 1 ? pair + s : s;
+    if (i & 1) sum += pair;
   }
-  return ordered((s[0] + s[1]) + (s[2] + s[3]));
+  return ordered(sum);
 }
 
 // A row's scores, one in 64 a lane: in registers (NV of them), or in LDS where there are more.
@@ -251,12 +265,7 @@ __device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float down, f
   for (int base = 0; base < open; base += 64 / LANES) {
     const int of = base + lane / LANES, b = __shfl(mine, of, 64);
     const u32x4 x = *reinterpret_cast<const u32x4*>(q + lane % LANES * 8), y = *reinterpret_cast<const u32x4*>(km + (long)b * DH + lane % LANES * 8);
-    double s = 0.0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s = __builtin_fma((double)__uint_as_float(x[e] << 16), (double)__uint_as_float(y[e] << 16), s);
-      s = __builtin_fma((double)__uint_as_float(x[e] & 0xffff0000u), (double)__uint_as_float(y[e] & 0xffff0000u), s);
-    }
+    double s = dot8(x, y);
 #pragma unroll
     for (int d = LANES / 2; d > 0; d /= 2) s += __shfl_xor(s, d, 64);
     if (lane % LANES == 0 && of < open) keys[of] = ordered(s);
