@@ -204,3 +204,33 @@ def test_attention_misses_no_block(H, Hk, dh, Lq, Lk, keep, entries):
             o = O.reshape(Lq, H, dh)[:, h, seen // 2 % dh]
             assert (share[:, seen] > 1.5 * _allowed(o, o)).all()
         _near(_attend(Q, K, V, lists, Lq, Lk, False), O, A)
+
+
+@pytest.mark.parametrize("H,dh,Lq,keep", [(2, 128, 130, 60), (3, 64, 1, 60), (20, 128, 300, 60)])
+def test_attention_joins_far_references(H, dh, Lq, keep):
+    """Slices whose logits are a hundred and more apart, up and down, slices of logits of -inf alone, and slices without a block."""
+    whole, slices = _plan(Lq, H, dh, keep)
+    assert whole == 0 and slices > 1
+    print(f"[case] attention_blocks far references H={H} dh={dh} Lq={Lq} keep={keep}: {slices} slices", flush=True)
+    rng = np.random.default_rng(dh + Lq)
+    nk = 64
+    Q = np.abs(_bf(rng.standard_normal((H, Lq, dh)))) + np.float32(2.0 ** -6)
+    Q[:, :, 0] = 8.0
+    Q = _bf(Q)
+    K, V = _bf(rng.standard_normal((H, nk * 64, dh))), _bf(rng.standard_normal((H, nk * 64, dh)))
+    K[:, :, 0] = np.repeat(_bf(rng.uniform(-128, 128, nk) * np.sqrt(dh) / 8), 64)
+    K[:, 5 * 64:21 * 64] = -np.inf
+    nq = -(-Lq // 128)
+    lists = np.full((H, nq, keep), -1)
+    for h in range(H):
+        for a in range(nq):
+            for e in range(slices):  # entry e, e + slices, ... are a slice's
+                kind = rng.integers(0, 4) if e else 3
+                at = np.arange(e, keep, slices)
+                of = np.r_[0:5, 21:nk] if kind == 3 else np.arange(5, 21) if kind else np.array([-1])
+                lists[h, a, at] = rng.choice(of, at.size)
+    lists[-1, -1] = rng.integers(5, 21, keep)  # -inf only: zeros
+    O, A = OB.attention_blocks(Q, K, V, lists, Lq, nk * 64)
+    got = _attend(Q, K, V, lists, Lq, nk * 64, False)
+    _near(got, O, A)
+    assert not got[(nq - 1) * 128:, -dh:].any()
