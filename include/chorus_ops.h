@@ -172,7 +172,8 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
  *         gain dev [dh] fp32, the same for every head
  *   pos   dev [L, n_axes] fp32: a token's coordinates (whole or not: stretched grids, shared text positions)
  *   freq, axis  dev [n_pairs] fp64 and int32: pair p turns by pos[axis[p]] * freq[p] radians, formed in fp64; a pair whose axis is
- *         outside [0, n_axes) does not turn. n_pairs <= dh / 2; the values behind the pairs pass through (normalised, not turned)
+ *         outside [0, n_axes) does not turn. n_pairs <= dh / 2; the values behind the pairs pass through (normalised, not turned). What
+ *         does not turn depends on what stands beside it by the norm alone, infinities and NaN included
  *   layout  CHORUS_ROPE_PAIRS: pair p is values 2p, 2p + 1 of a head; _HALVES: values p, n_pairs + p (n_pairs % 8 == 0)
  *   out   dev bf16 [H, Lpad, dh]; rows L..Lpad-1 are written as zeros; must not overlap `in`
  *   out_scale  as chorus_qk_norm_rope
@@ -189,19 +190,20 @@ int32_t chorus_attention_slices_plan(int64_t L, int32_t H, int32_t dh, int32_t c
  *   dh/32, ..., 1
  *   rule   dev uint8 [nk] or NULL: 1 = ahead of all others, 2 = never, anything else by its score
  *   blocks dev int32 [H, nq, keep]: ascending, -1 behind the last
- *   nk from 1 to CHORUS_BLOCK_SELECT_MAX, nq * H at most 2^22 - 1 (CHORUS_E_SHAPE), keep >= 1.
+ *   nk from 1 to CHORUS_BLOCK_SELECT_MAX, nq * H at most 2^22 - 1, keep at most 2^31 - 65 (CHORUS_E_SHAPE), keep >= 1 (CHORUS_E_ARG).
  *
  * chorus_attention_blocks: O = softmax(Q K^T / sqrt(dh)) V with the queries of block a (CHORUS_BLOCK_QUERIES of them) of head h seeing
  *   the keys of the key blocks (CHORUS_BLOCK_KEYS keys) in blocks[h, a, :] only. An entry outside [0, ceil(Lk / 64)) is passed over, so
  *   -1 fills a shorter list; the order does not matter but to the rounding; a block that is listed twice counts twice. A row that sees
- *   no key, or only logits of -inf, is zeros. Keys and values that no list names are not read.
+ *   no key, or only logits of -inf, is zeros. Keys and values that no list names are not read. Logits, sums and results are fp32; the
+ *   weights are rounded to bf16 for the matrix pipe, as in chorus_attention, and their sum is that of the rounded ones.
  *   Q dev bf16 [H, LqPad, dh], K dev bf16 [Hk, LkPad, dh], Vt dev bf16 [Hk*dh, LkPad] in chorus_v_transpose's layout
  *   (H % Hk == 0; head h reads h / (H / Hk)), O dev bf16 [Lq, H*dh], blocks dev int32 [H, ceil(Lq / 128), keep]
  *   prescaled  non-zero: Q holds the queries multiplied by CHORUS_ATTENTION_Q_PRESCALE(dh), as for chorus_attention's variant 6
  *   ws    dev, chorus_attention_blocks_workspace_bytes bytes (0: none, ws may be NULL): the fp32 results of lists that are cut so that few
  *         of them fill the GPU. Scratch of this call alone: calls that may run at the same time need one each
- *   dh in {64,128}; LkPad % 64 == 0, 2^22 >= LkPad >= Lk >= 1; at most 2^24 - 2^15 - 2 lists (H * ceil(Lq / 128)); rows and columns
- *   beyond Lq and Lk are padding (finite values).
+ *   dh in {64,128}; LkPad % 64 == 0, 2^22 >= LkPad >= Lk >= 1; at most 2^24 - 2^15 - 2 lists (H * ceil(Lq / 128)) of 2^31 - 65
+ *   entries; rows and columns beyond Lq and Lk are padding (finite values).
  * Errors: CHORUS_E_ARG, CHORUS_E_SHAPE, CHORUS_E_WORKSPACE, CHORUS_E_HIP.
  * ------------------------------------------------------------------------ */
 #define CHORUS_ROPE_NORM_NONE 0

@@ -1,20 +1,26 @@
-// Attention over listed blocks of keys: O = softmax(Q K^T / sqrt(dh)) V, a query seeing the keys of the blocks in the list of its block of
-// 128 queries and head, and no others. bf16 operands on the matrix pipe, fp32 online softmax, logits never leave registers.
+// Attention over listed blocks of keys: O = softmax(Q K^T / sqrt(dh)) V, a query seeing the keys of the blocks in the list of its
+// block of 128 queries and head, and no others. bf16 operands on the matrix pipe, fp32 online softmax, logits never leave
+// registers.
 //
-// A workgroup of four waves takes a list: a wave holds 32 of the 128 queries (two blocks of 16, in registers) and all walk over the list a
-// block of 64 keys at a time, in tiles in LDS. A compute unit holds two workgroups, a wave of each on every SIMD. They get half a step apart by
-// themselves, the matrix phase going ahead of the other's vector phase: while the waves of one make the weights of a tile on the vector pipe, those
-// of the other keep the matrix pipe busy (O += V P, then the next tile's S = K Q^T). Held apart by barriers across both, as one workgroup with
-// two lists, they are no faster where lists are alike (32760 queries 1026 us, 1014 as they are) and wait for each other where they are not
-// (13104 queries with 30 to 60 blocks, 12 heads: 236 us, 215). Neighbouring lists meet many of the same blocks, which then come from the L2.
+// A workgroup of four waves takes a list: a wave holds 32 of the 128 queries (two blocks of 16, in registers) and all walk over the
+// list a block of 64 keys at a time, in tiles in LDS. A compute unit holds two workgroups of heads of 128, a wave of each on every
+// SIMD (and four of heads of 64, which take 120 to 128 registers and 32 KB). They get half a step apart by themselves, the matrix
+// phase going ahead of the other's vector phase: while the waves of one make the weights of a tile on the vector pipe, those of the
+// other keep the matrix pipe busy (O += V P, then the next tile's S = K Q^T). Held apart by barriers across both, as one workgroup
+// with two lists, they are no faster where lists are alike (32760 queries 1026 us, 1014 as they are) and wait for each other where
+// they are not (13104 queries with 30 to 60 blocks, 12 heads: 236 us, 215). Neighbouring lists meet many of the same blocks, which
+// then come from the L2.
 //
-// What a step has to fit into: 68 MFMAs a wave (1088 cycles of the pipe), 32 exponentials (512) and about 90 other vector instructions.
-// Measured (cycles a step, 32760 queries, 103 blocks each, 12 heads): vector phase 1240, matrix phase 1435, so the matrix pipe is busy
-// three quarters of the time at the clock that the power management leaves; 1014 us, 1310 TFLOP/s, where the dense kernel has 1380 over 13184
-// keys and 1170 over as many as these lists hold (all three a few percent apart from card to card). The probabilities are rounded to bf16 for
-// the matrix pipe, once, and their sum is taken over the rounded ones. On the way there: the next logits made beside the
-// exponentials of this tile 1165 (the two pipes hardly overlap inside a wave); loops that were unrolled by two for constant buffer
-// addresses 1060 (the register allocator gives every MFMA result a new home then, and reads wait for the old ones).
+// What a step has to fit into: 68 MFMAs a wave (1088 cycles of the pipe), 32 exponentials (512) and about 90 other vector
+// instructions. Measured (cycles a step, 32760 queries, 103 blocks each, 12 heads): vector phase 1240, matrix phase 1435, so the
+// matrix pipe is busy three quarters of the time at the clock that the power management leaves; 1014 us, 1310 TFLOP/s, where the
+// dense kernel has 1380 over 13184 keys and 1170 over as many as these lists hold (all three a few percent apart from card to
+// card). Queries that are not scaled before cost 32 multiplications a step more, 1085 us where scaled ones took 1046 on the same
+// card. Heads of 64 have half the MFMAs but all the exponentials: 590 us and 633 unscaled, 1124 TFLOP/s, the vector pipe issuing 70
+// % of the time (52 with heads of 128) and the matrix pipe busy 63 % (72). The probabilities are rounded to bf16 for the matrix
+// pipe, once, and their sum is taken over the rounded ones. On the way there: the next logits made beside the exponentials of this
+// tile 1165 (the two pipes hardly overlap inside a wave); loops that were unrolled by two for constant buffer addresses 1060 (the
+// register allocator gives every MFMA result a new home then, and reads wait for the old ones).
 //
 // The operand layouts are those of the dense kernel on v_mfma_f32_16x16x32_bf16: S^T = K Q^T leaves a lane with the logits of one query
 // row, and in the order in which V^T is stored (chorus_v_transpose) its probabilities are the B operand of O^T += V^T P^T as they stand:
@@ -37,10 +43,13 @@ struct BlockPlan {
   long whole;
   int cut, slices;
 };
-// Lists that leave the last round of workgroups (two on a compute unit) partly empty, or the only one, are cut into as many slices as make that
-// round the shortest. A block takes a workgroup of heads of 128 about 1.2 us alone on its unit and 1.5 beside another, heads of 64 seven tenths of
-// that; a slice costs its fp32 result on the way out and in (3 TB/s), the join 8 us. us, lists of blocks, dh: 40 of 118, 128: 6 slices 36, 1 124, 12
-// 40; 32 of 30, 64: 6 slices 15, 1 26, 16 20; 256 of 100, 128: 2 slices 97, 1 122, 4 107; 312 of 20, 128: whole 36, 2 slices 49.
+// Lists that leave the last round of workgroups (two on a compute unit) partly empty, or the only one, are cut into as many slices
+// as make that round the shortest. A block takes a workgroup of heads of 128 about 1.2 us alone on its unit and 1.5 beside another,
+// heads of 64 seven tenths of that, with two counted to a unit though four fit: the more there are the longer a step of each takes,
+// and counted as four the cut comes out worse (us, lists of blocks: 600 of 100 126 as it is, 146 with four; 516 of 200 210, 237;
+// 768 of 60 102, 96). A slice costs its fp32 result on the way out and in (3 TB/s), the join 8 us. us, lists of blocks, dh: 40 of
+// 118, 128: 6 slices 36, 1 124, 12 40; 32 of 30, 64: 6 slices 15, 1 26, 16 20; 256 of 100, 128: 2 slices 97, 1 122, 4 107; 312 of
+// 20, 128: whole 36, 2 slices 49.
 BlockPlan block_plan(long lists, int dh, int keep) {
   constexpr long units = 256, places = 2 * units;
   const long cut = lists % places;
@@ -159,7 +168,8 @@ __global__ __launch_bounds__(256, 2) void attention_blocks_kernel(const uint16_t
   bf16x8 qf[RB][KC];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    // four neighbouring lanes read 64 bytes of a row, which is a request; what they hold is another lane's, where lq % 4 and g change places
+    // four neighbouring lanes read 64 bytes of a row, which is a request; what they hold is another lane's, where lq % 4 and g
+    // change places
     long q = (long)qb * BQ + wave * 32 + 16 * rb + (lq & 12) + g;
     if (q > Lq - 1) q = Lq - 1;
     const uint16_t* qp = Q + ((long)head * LqPad + q) * DH + 8 * (lq & 3);
@@ -290,7 +300,8 @@ __global__ __launch_bounds__(256, 2) void attention_blocks_kernel(const uint16_t
     b1 = b2;
     if (b1 >= 0) b2 = list.next();
     __builtin_amdgcn_sched_barrier(0);
-    // this tile's values and the next one's keys, requested a step ago, are in LDS for all four waves; the keys requested above are not waited for
+    // this tile's values and the next one's keys, requested a step ago, are in LDS for all four waves; the keys requested above are
+    // not waited for
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(K_LD) : "memory");
     __builtin_amdgcn_sched_barrier(0);
     // ================= matrix phase: this tile's share of the result, and the logits of the next one =================
@@ -358,7 +369,8 @@ __global__ __launch_bounds__(256, 2) void attention_blocks_kernel(const uint16_t
       const int src = 16 * (b4 >> 1 | (b4 & 1) << 1) + (lq & 12) + g;
 #pragma unroll
       for (int i = 0; i < DB / 2; ++i) {
-        // 4 values of block 2i and 4 of 2i + 1 here, and as many with the lane 16 further: after the swap eight of the one here, of the other there
+        // 4 values of block 2i and 4 of 2i + 1 here, and as many with the lane 16 further: after the swap eight of the one here, of
+        // the other there
         const f32x4 x = o[2 * i][rb] * inv, y = o[2 * i + 1][rb] * inv;
         const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[0], x[1]), pack_bf16x2(y[0], y[1]), false, false);
         const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[2], x[3]), pack_bf16x2(y[2], y[3]), false, false);
@@ -370,9 +382,9 @@ __global__ __launch_bounds__(256, 2) void attention_blocks_kernel(const uint16_t
 #endif
 }
 
-// Puts the slices of a row together, W waves a row: the largest reference, then the slices' results and sums by their distance from it, in an order that
-// depends on nothing but their number. Bound by the way to them: with one wave a row, its 42 slices were 10 reads one behind the other (60 rows, 12
-// heads 10.4 us).
+// Puts the slices of a row together, W waves a row: the largest reference, then the slices' results and sums by their distance from
+// it, in an order that depends on nothing but their number. Bound by the way to them: with one wave a row, its 42 slices were 10
+// reads one behind the other (60 rows, 12 heads 10.4 us).
 template <int DH, int W>
 __global__ __launch_bounds__(256) void attention_blocks_join_kernel(const float* __restrict__ part, uint16_t* __restrict__ O, long Lq, int H, int nq,
                                                                     int whole, int slices, int cut, float scale_log2) {
@@ -392,7 +404,6 @@ __global__ __launch_bounds__(256) void attention_blocks_join_kernel(const float*
   const float total = wave_sum(w * ml.y);
   const float inv = total == 0.f ? 0.f : 1.0f / total;
   float sum[E] = {};
-#pragma unroll 8
   for (int s = share; live && s < slices; s += W) {
     const float* p = part + (first + (long)s * BQ) * DH + E * lane;
     const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
@@ -472,7 +483,8 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
 #undef ATTEND
   CHORUS_LAUNCH_CHECK();
   if (need) {
-    // Four waves a row as long as all of them are on the GPU at once (32 a unit): 12 lists in 12 slices 15.0 us the call, 17.6 with one; 40 lists 23.0, 21.5.
+    // Four waves a row as long as all of them are on the GPU at once (32 a unit): 12 lists in 12 slices 15.0 us the call, 17.6 with
+    // one; 40 lists 23.0, 21.5.
     const int waves = p.cut * BQ * 4 <= 256 * 32 && p.slices >= 4 ? 4 : 1;
     const dim3 join((unsigned)(p.cut * (BQ / 4 * waves)));
 #define JOIN(DH, W)                                                                                                                      \

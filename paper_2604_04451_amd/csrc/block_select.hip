@@ -5,9 +5,10 @@
 namespace chorus {
 namespace {
 
-// Mean over blocks of BLOCK consecutive rows of a head, a wave a block: a lane sums one chunk of eight values of every 64 / (dh / 8)-th
-// row, each divided by BLOCK ahead of the sum, which is exact and keeps sums of the largest values finite, then the lanes of a chunk are added. HBM-bound: each row is read once, 16 bytes a lane, eight rows of a lane in flight (75600 x 5120 135 us,
-// 5.8 TB/s; 3271 x 1536 3.9 us, with one behind the other, where few blocks wait a memory latency a row, 6.8).
+// Mean over blocks of BLOCK consecutive rows of a head, a wave a block: a lane sums one chunk of eight values of every 64 / (dh /
+// 8)-th row, each divided by BLOCK ahead of the sum, which is exact and keeps sums of the largest values finite, then the lanes of
+// a chunk are added. HBM-bound: each row is read once, 16 bytes a lane, eight rows of a lane in flight (75600 x 5120 135 us, 5.8
+// TB/s; 3271 x 1536 3.9 us, with one behind the other, where few blocks wait a memory latency a row, 6.8).
 template <int DH, int BLOCK>
 __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restrict__ X, uint16_t* __restrict__ out, long L, long Lpad,
                                                          long nb, long total) {
@@ -72,8 +73,9 @@ __global__ __launch_bounds__(256) void block_mean_kernel(const uint16_t* __restr
 //
 // How far a score can be off: products of bf16 are exact in fp32, and whatever the order of a sum of DH <= 128 of them, each of its
 // additions is off by at most 2^-23 of the sum of magnitudes, itself at most |q| |k|: kBound |q| max |k|, and a trace for values
-// that are flushed. Norms come from the same pipe (the largest entry of K K^T, which is on its diagonal) and are within 2^-16 of their values, which kBound has room for.
-// Where |q| |k| is a number below 1e38 every score is one; where it is not (infinities, NaN, sums that fp32 does not hold) all scores are made in fp64.
+// that are flushed. Norms come from the same pipe (the largest entry of K K^T, which is on its diagonal) and are within 2^-16 of
+// their values, which kBound has room for. Where |q| |k| is a number below 1e38 every score is one; where it is not (infinities,
+// NaN, sums that fp32 does not hold) all scores are made in fp64.
 //
 // Two fifths of a workgroup's time go into the sweep over the keys (20K of 48K cycles at 591 x 1182 blocks, 40 heads: 77 us), the rest into its
 // rows; there the vector and the scalar pipe share the work, 20 comparisons and 40 counts for each look at a row. The search therefore stays
@@ -136,6 +138,11 @@ __device__ __forceinline__ uint64_t exact_score(const uint16_t* __restrict__ q, 
   return ordered(sum);
 }
 
+// Loops over a lane's scores that count across the wave: unrolled where the scores are in registers; in LDS, of a length not known
+// before, they cannot be.
+template <int NV>
+constexpr int kTimesOf = NV > 0 ? NV : 1;
+
 // A row's scores, one in 64 a lane: in registers (NV of them), or in LDS where there are more.
 template <int NV>
 struct Scores {
@@ -159,15 +166,16 @@ struct Scores {
         for (int j = 0; j < 8; ++j) c += __builtin_popcountll(__ballot(x[j] >= t));
       }
     }
-#pragma unroll
+#pragma unroll kTimesOf<NV>
     for (; i < count(); ++i) c += __builtin_popcountll(__ballot(get(i) >= t));
     return c;
   }
-  // Where the border of the W largest is, `in` of the scores being +inf and `all` not -inf: `reached` of them reach `low`, W or more, and fewer than W
-  // lie above `high`. Bisection between -bound and bound, beyond which there are finite scores on neither side: first at twice the usual
-  // size of a score and at 0, then in the middle (a row's scores are spread like a bell, and halves of their range come near in a few
-  // steps), until W are left above, or no more is to be had from scores that are `off` from exact. As soon as the border lies among 64 scores
-  // or fewer they move to a lane each, and a step costs one comparison. With W reached low = high is the W-th score, and `next` the one behind.
+  // Where the border of the W largest is, `in` of the scores being +inf and `all` not -inf: `reached` of them reach `low`, W or
+  // more, and fewer than W lie above `high`. Bisection between -bound and bound, beyond which there are finite scores on neither
+  // side: first at twice the usual size of a score and at 0, then in the middle (a row's scores are spread like a bell, and halves
+  // of their range come near in a few steps), until W are left above, or no more is to be had from scores that are `off` from
+  // exact. As soon as the border lies among 64 scores or fewer they move to a lane each, and a step costs one comparison. With W
+  // reached low = high is the W-th score, and `next` the one behind.
   struct Border {
     float low, high, next;
     int reached;
@@ -195,7 +203,7 @@ struct Scores {
       }
     } else if (reach_lo - reach_hi <= 64) {
       int at = 0;
-#pragma unroll
+#pragma unroll kTimesOf<NV>
       for (int i = 0; i < count(); ++i) {
         const float x = get(i);
         const bool of = x >= lo && x < hi;
@@ -225,10 +233,10 @@ struct Scores {
 };
 
 // Writes a row's choice, the blocks whose `take` holds: ascending, then -1.
-template <class TAKE>
+template <int NV, class TAKE>
 __device__ __forceinline__ void put_row(int n, TAKE take, int* __restrict__ to, int keep, int lane) {
   int put = 0;
-#pragma unroll
+#pragma unroll kTimesOf<NV>
   for (int i = 0; i < n; ++i) {
     const bool t = take(i);
     const uint64_t taken = __ballot(t);
@@ -238,16 +246,16 @@ __device__ __forceinline__ void put_row(int n, TAKE take, int* __restrict__ to, 
   for (int i = put + lane; i < keep; i += 64) to[i] = -1;
 }
 
-// The scores from `down` to `up`, which the others leave open, kMostOpen of them at most, become +inf or -inf by their exact values: 8 values of a row
-// a lane, so 8 or 16 lanes a block make its score, which is two reads and a sum away; then each open block's lane counts those in front.
-// Returns false, with nothing done, where more are open.
+// The scores from `down` to `up`, which the others leave open, kMostOpen of them at most, become +inf or -inf by their exact
+// values: 8 values of a row a lane, so 8 or 16 lanes a block make its score, which is two reads and a sum away; then each open
+// block's lane counts those in front. Returns false, with nothing done, where more are open.
 constexpr int kMostOpen = 32;
 template <int DH, int NV>
 __device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float down, float up, uint64_t* __restrict__ keys, const uint16_t* __restrict__ q,
                                              const uint16_t* __restrict__ km, int lane) {
   uint32_t* list = reinterpret_cast<uint32_t*>(keys);
   int open = 0, before = 0;
-#pragma unroll
+#pragma unroll kTimesOf<NV>
   for (int i = 0; i < v.count(); ++i) {
     const float x = v.get(i);
     before += __builtin_popcountll(__ballot(x > up));
@@ -280,7 +288,7 @@ __device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float down, f
   const uint64_t kept = __ballot(lane < open && before < W);
   __builtin_amdgcn_wave_barrier();
   open = 0;
-#pragma unroll
+#pragma unroll kTimesOf<NV>
   for (int i = 0; i < v.count(); ++i) {
     const float x = v.get(i);
     const uint64_t mask = __ballot(x >= down && x <= up);
@@ -291,7 +299,8 @@ __device__ __forceinline__ bool close_border(Scores<NV>& v, int W, float down, f
   return true;
 }
 
-// The choice of W where fp32 scores say nothing (`odd`), or are as good as equal by the dozen, from `down` to `up`. It is rare, works in LDS and stays out of the row loop's registers. The row there holds scores (+inf: in, -inf: out).
+// The choice of W where fp32 scores say nothing (`odd`), or are as good as equal by the dozen, from `down` to `up`. It is rare,
+// works in LDS and stays out of the row loop's registers. The row there holds scores (+inf: in, -inf: out).
 template <int DH>
 __device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, int W, bool odd, float down, float up, const uint16_t* __restrict__ q,
                                              const uint16_t* __restrict__ km, int* __restrict__ to, int keep, int lane) {
@@ -342,7 +351,7 @@ __device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, i
       if (x != kOut && x != kIn && x != tied) at[64 * i] = x > tied ? kIn : kOut;
     }
   }
-  put_row(n, [&](int i) {
+  put_row<0>(n, [&](int i) {
     const uint32_t x = at[64 * i];
     const uint64_t ties = __ballot(tied != kOut && x == tied);
     const bool take = x >= from || (tied != kOut && x == tied && lanes_below(ties, 0) < equal);
@@ -351,7 +360,10 @@ __device__ __noinline__ void put_row_exactly(uint32_t* __restrict__ at, int n, i
   }, to, keep, lane);
 }
 
-// T: 16-row tiles of queries, R = 16 T rows or fewer where T is 1. THREADS: 1024 where a lane's scores fit the registers of four waves a SIMD.
+// T: 16-row tiles of queries, R = 16 T rows or fewer where T is 1. THREADS: 1024, four waves a SIMD of 128 registers a lane, but
+// where a lane holds 40 scores. With 20 it takes a little more than there are: 1 to 9 values of a lane wait in scratch memory (16
+// to 48 bytes), written once ahead of the sweep over the keys and read once behind it, and 71 scalar values in lanes of vector
+// registers (188 with 40 scores, 22 with 8).
 template <int DH, int NV, int T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select_kernel(const uint16_t* __restrict__ Qm, const uint16_t* __restrict__ Km,
                                                                                         const uint8_t* __restrict__ rule, int* __restrict__ blocks, int nq,
@@ -373,9 +385,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   for (int i = 0; i < (NV > 0 ? NV : 1); ++i) of_block[i] = rule_of(i);
   {
     const int l16 = lane & 15, g = lane >> 4;
-    // A lane's KC fragments are neighbouring pieces of 16 bytes of its row. Read as they stand, each lane would be a request of its own, which is
-    // what the sweep then waits for (591 x 1182 blocks, 40 heads, 91 us instead of 77; 256 x 512, 12 heads, 14.8 instead of 11.8); so KC
-    // neighbouring lanes read the pieces of one row, KC rows in turn, and exchange them.
+    // A lane's KC fragments are neighbouring pieces of 16 bytes of its row. Read as they stand, each lane would be a request of its
+    // own, which is what the sweep then waits for (591 x 1182 blocks, 40 heads, 91 us instead of 77; 256 x 512, 12 heads, 14.8
+    // instead of 11.8); so KC neighbouring lanes read the pieces of one row, KC rows in turn, and exchange them.
     const int r0 = l16 / KC * KC, piece = KC * g + l16 % KC;
     bf16x8 qf[T][KC];
 #pragma unroll
@@ -460,7 +472,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   int always = 0, ordinary = nk;
   if (rule) {
     ordinary = 0;
-#pragma unroll
+#pragma unroll kTimesOf<NV>
     for (int i = 0; i < n; ++i) {
       const uint32_t c = NV > 0 ? of_block[NV > 0 ? i : 0] : rule_of(i);
       always += __builtin_popcountll(__ballot(c == 1));
@@ -507,7 +519,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
       }
     }
     if (clear) {
-      put_row(v.count(), [&](int i) { return v.get(i) >= from; }, to, keep, lane);
+      put_row<NV>(v.count(), [&](int i) { return v.get(i) >= from; }, to, keep, lane);
     } else {
 #pragma unroll
       for (int i = 0; i < v.count(); ++i)
@@ -517,10 +529,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 2) void block_select
   }
 }
 
-// The rows of a workgroup. All of them share one sweep over a head's keys, which is what the call waits for (1182 blocks of 128 values are 300 KB, from
-// the L2, and a compute unit holds one workgroup): as few as let the launch run in one round of workgroups, and where it takes more than
-// one, 32 (two matrix tiles) or as many as their scores leave room for in the LDS, down to two rows of CHORUS_BLOCK_SELECT_MAX scores
-// (128 KB). 103 x 205 blocks, 12 heads: 8 rows 9.2 us, 4 rows (312 workgroups) half as long again.
+// The rows of a workgroup. All of them share one sweep over a head's keys, which is what the call waits for (1182 blocks of 128
+// values are 300 KB, from the L2, and a compute unit holds one workgroup): as few as let the launch run in one round of workgroups,
+// and where it takes more than one, 32 (two matrix tiles) or as many as their scores leave room for in the LDS, down to two rows of
+// CHORUS_BLOCK_SELECT_MAX scores (128 KB). 103 x 205 blocks, 12 heads: 8 rows 9.2 us, 4 rows (312 workgroups) half as long again.
 int select_rows(long nq, int H, int stride) {
   int R = 4;
   while (R < 32 && (nq + R - 1) / R * H > 256) R *= 2;
@@ -583,7 +595,10 @@ int32_t chorus_block_select(const uint16_t* Qm, const uint16_t* Km, const uint8_
     if (R == 32) SELECT(DH, NV, 2, THREADS);   \
     else SELECT(DH, NV, 1, THREADS);           \
   } while (0)
-  // A row's scores stay in registers up to 40 a lane; behind that they are read from LDS at each look (2 rows of 9000 blocks: 109 us).
+  // A lane holds the scores of its row in 8, 20 or 40 registers, the fewest of these that do, and behind that reads them from LDS
+  // at each look (2 rows of 9000 blocks: 88 us). At the borders, 12 heads: 256 rows of 512 blocks 11.1 us with 8 registers, 16.6
+  // with 20; 600 of 1280 37.4 with 20, 64.0 with 40; 600 of 2560 104 with 40, 141 from LDS. More steps would pay between them: 300
+  // rows of 600 blocks 17.5 us, 13.3 with 12 registers; 450 of 1000 27.5, 24.4 with 16.
 #define SELECT_LENGTH(DH)                           \
   do {                                              \
     if (nk <= 64 * 8) SELECT_ROWS(DH, 8, 1024);     \

@@ -40,9 +40,10 @@ __device__ __forceinline__ float sum_squares(const float (&x)[8]) {
   return s;
 }
 
-// A wave a token; a lane takes chunks of eight values, so a head is 8 or 16 neighbouring lanes. HBM-bound: each row is read once and written once.
-// NCH > 0: rows of more than 512 FULL and up to 512 NCH values, whose loads are all issued ahead of the angles and which stay in registers; NCH == 0:
-// any number of heads, chunk by chunk, and twice (the second time from the cache) where the norm is over the row.
+// A wave a token; a lane takes chunks of eight values, so a head is 8 or 16 neighbouring lanes. HBM-bound: each row is read once
+// and written once. NCH > 0: rows of more than 512 FULL and up to 512 NCH values, whose loads are all issued ahead of the angles
+// and which stay in registers; NCH == 0: any number of heads, chunk by chunk, and twice (the second time from the cache) where the
+// norm is over the row.
 template <int NORM, bool HALVES, int NCH, int FULL>
 __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restrict__ in, long ld, const float* __restrict__ gain,
                                                         uint16_t* __restrict__ out, long L, long Lpad, int H, int dh,
@@ -80,7 +81,9 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     s_sin[wave][lane] = sn;
     __builtin_amdgcn_wave_barrier();
   }
-  float rstd = 1.0f;  // with out_scale in it; where there is no norm, out_scale is the gain: ahead of the rotation, which may leave fp32 without it
+  // With out_scale in it. Where there is no norm, out_scale is the gain and goes in ahead of the rotation, whose values fp32 may not
+  // hold without it.
+  float rstd = 1.0f;
   if (NORM == CHORUS_ROPE_NORM_WIDTH) {
     float ss = 0.f, x[8];
     if (NCH > 0) {
@@ -99,9 +102,11 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     rstd = rsqrtf(wave_sum(ss) / (float)(H * dh) + kEps) * out_scale;
   }
   const int iters = NCH > 0 ? NCH : (nchunk + 63) / 64;
+  constexpr int kTimes = NCH > 0 ? NCH : 1;
   const int d0 = lane % lanes * 8;  // in its head, whatever the chunk
-  // Halves: a value's other half is in a lane of the same head, `off` values further. Gains go in ahead of the rotation and the norm behind it, where
-  // a value takes it once (75600 x 5120, norm of the head 300 us, both halves normalised ahead 330; norm of the row 302 and 337).
+  // Halves: a value's other half is in a lane of the same head, `off` values further. Gains go in ahead of the rotation and the
+  // norm behind it, where a value takes it once (75600 x 5120, norm of the head 300 us, both halves normalised ahead 330; norm of
+  // the row 302 and 337).
   const bool first = d0 < n_pairs;
   const int off = !HALVES || d0 >= 2 * n_pairs ? 0 : first ? n_pairs : -n_pairs;
   const uint32_t turns = HALVES ? (off != 0 ? (uint32_t)(turning >> (first ? d0 : d0 - n_pairs)) : 0u) : (uint32_t)(turning >> (d0 >> 1));
@@ -114,7 +119,7 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
       sn[e] = off == 0 ? 0.f : first ? -s_sin[wave][p + e] : s_sin[wave][p + e];
     }
   }
-#pragma unroll
+#pragma unroll kTimes
   for (int it = 0; it < iters; ++it) {
     const int c0 = 64 * it;
     const bool live = it < FULL || c0 + lane < nchunk;
@@ -130,7 +135,8 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const uint16_t* __restri
     auto gains = [&](float(&v)[8], int at) {
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
-        const f32x4 q = NORM == CHORUS_ROPE_NORM_NONE ? f32x4{out_scale, out_scale, out_scale, out_scale} : *reinterpret_cast<const f32x4*>(g + at + e);
+        const f32x4 q = NORM == CHORUS_ROPE_NORM_NONE ? f32x4{out_scale, out_scale, out_scale, out_scale}
+                                                      : *reinterpret_cast<const f32x4*>(g + at + e);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[e + i] = q[i];
       }
@@ -222,8 +228,8 @@ int32_t chorus_rope_axes(const uint16_t* in, int64_t ld, const float* gain, int3
 #define ROPE_ROWS(NORM, HALVES, NCH, FULL)                                                                                              \
   hipLaunchKernelGGL((rope_axes_kernel<NORM, HALVES, NCH, FULL>), dim3((unsigned)((Lpad + 3) / 4)), dim3(256), 0, (hipStream_t)stream, in, \
                      (long)ld, gain, out, (long)L, (long)Lpad, H, dh, pos, n_axes, freq, axis, n_pairs, out_scale)
-  // by the width alone: up to 40 registers of a row, in steps that leave at most 3 of 10 chunks empty (20000 rows of 26 heads of 128 and their
-  // norm: 53.5 us, chunk by chunk 63.3; 32760 rows of 12 heads 34.9)
+  // by the width alone: up to 40 registers of a row, in steps that leave at most 3 of 10 chunks empty (20000 rows of 26 heads of
+  // 128 and their norm: 53.5 us, chunk by chunk 63.3; 32760 rows of 12 heads 32.6)
 #define ROPE(NORM, HALVES)                                  \
   do {                                                      \
     if (D <= 512) ROPE_ROWS(NORM, HALVES, 1, 0);            \
