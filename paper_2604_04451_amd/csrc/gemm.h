@@ -30,4 +30,24 @@ int32_t gemm_bf16_two(const uint16_t* A, const uint16_t* W, int64_t M, int32_t N
                       const uint16_t* A2, const uint16_t* W2, int64_t M2, int32_t N2, uint16_t* out2, const float* bias2,
                       void* stream);
 
+// a tile's bytes, 256 rows of 2 K, within the 32-bit offsets of its loads; longer rows are 64 x 64 tiles' alone
+constexpr int kMaxOffsetK = (1 << 22) - 64;
+
+// the tile kernels by their shapes
+enum Tile { kTile256, kTileWide, kTile128, kTile128Deep, kTile64, kTiles };
+constexpr int kTileNumber[kTiles] = {3, 2, 4, 5, 1};  // as chorus_gemm_bf16_kernel names them
+constexpr int kTileRows[kTiles] = {256, 128, 128, 128, 64};
+constexpr int kTileCols[kTiles] = {256, 256, 128, 128, 64};
+// half steps in LDS of the deep 128 x 128 and of the 64 x 64 tiles
+constexpr int kHalvesDeep = 7, kHalves64 = 9;
+
+// On which tiles a whole product (no slices) is the fastest by the estimates for bf16: the first head_rows rows on kTile256 in a launch
+// of their own (0: none), the others on `tile`. What is estimated is the operands' way into the compute units, so that products of other
+// types go by it too, with K in units of 2 bytes and N the rows of all weight matrices.
+struct TileCut {
+  long head_rows;
+  int tile;
+};
+TileCut gemm_tiles(int64_t M, int32_t N, int32_t K, int32_t epilogue);
+
 }  // namespace chorus
