@@ -227,6 +227,51 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
                                 void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Products of 8-bit integers with a scale for each token and each output channel, for projections that are served from quantised
+ * weights; what chorus_gemm_bf16 is for bf16 ones, with the same epilogues.
+ *
+ * chorus_quant_rows_i8: scale[m] = max|x[m]| / 127 (fp32), out[m][k] = 127 x[m][k] / max|x[m]| to the nearest whole number, halves to even
+ *   (as if the quotient were exact). Tokens before a product, and the rows of a weight matrix once.
+ *   X     dev bf16, row m at X + m*ld, K values (K % 8 == 0, ld >= K, ld % 8 == 0)
+ *   out   dev int8 [M, Kp], zeros behind K (Kp >= K, Kp % 8 == 0; chorus_gemm_i8 wants a multiple of 128)
+ *   scale dev fp32 [M]; a row of zeros has scale 0, one that holds an infinity or NaN has scale NaN; the codes of both are zeros
+ *   M at most 2^23 - 1 (CHORUS_E_SHAPE).
+ *
+ * chorus_gemm_i8: out = epilogue((sum_k A[m][k] W[n][k]) * a_scale[m] * w_scale[n] + bias[n])
+ *   A dev int8 [M, K], W dev int8 [N, K], a_scale dev fp32 [M], w_scale dev fp32 [N]; any codes, -128 included. The sums are exact.
+ *   epilogue, out, bias, gate0, gate1, scale: as chorus_gemm_bf16
+ *   K % 128 == 0, K <= 131072, N % 8 == 0 (CHORUS_E_SHAPE); M >= 0 arbitrary.
+ * ------------------------------------------------------------------------ */
+int32_t chorus_quant_rows_i8(const uint16_t* X, int64_t ld, int8_t* out, float* scale, int64_t M, int32_t K, int32_t Kp, void* stream);
+int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int64_t M, int32_t N, int32_t K,
+                       int32_t epilogue, void* out, const float* bias, const float* gate0, const float* gate1, float scale, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The gated half of a feed-forward block, as text encoders have it, and its gradients: h = act(x Wg^T) * (x Wu^T). The product with the
+ * second matrix is chorus_gemm_bf16's.
+ *   X   dev bf16 [M, K]
+ *   W   dev bf16 [2 F, K]: the F rows of the gate, then those of the other factor
+ *   act CHORUS_ACT_GELU (tanh form, as the block's) or CHORUS_ACT_SILU
+ *   H   dev bf16 [M, F]; both projections stay in fp32 until their product is rounded
+ *   pre dev bf16 [M, 2 F] or NULL: both projections, rounded, for the backward pass
+ *
+ * chorus_gated_ffn_backward: from dH (dev bf16 [M, F], the gradient of H) and pre,
+ *   dX  dev bf16 [M, K] or NULL
+ *   dW  dev [2 F, K] or NULL; dw_epilogue: CHORUS_EPI_BF16 (bf16), CHORUS_EPI_F32 (fp32) or CHORUS_EPI_RESID (fp32, added to what stands
+ *       there: gradients of several batches)
+ *   The gradients of the projections are rounded to bf16, the operand type of the matrix pipe.
+ *   ws  dev, chorus_gated_ffn_backward_workspace_bytes(M, F, K) bytes, scratch of this call alone
+ *   Outputs must not overlap inputs. M == 0: CHORUS_E_SHAPE (the forward pass accepts it and does nothing).
+ * K % 64 == 0, F % 64 == 0, both at most 2^20, M at most 2^22 (CHORUS_E_SHAPE).
+ * ------------------------------------------------------------------------ */
+#define CHORUS_ACT_GELU 0
+#define CHORUS_ACT_SILU 1
+int32_t chorus_gated_ffn(const uint16_t* X, const uint16_t* W, int32_t act, uint16_t* H, uint16_t* pre, int64_t M, int32_t F, int32_t K, void* stream);
+size_t chorus_gated_ffn_backward_workspace_bytes(int64_t M, int32_t F, int32_t K);
+int32_t chorus_gated_ffn_backward(const uint16_t* X, const uint16_t* W, const uint16_t* pre, const uint16_t* dH, int32_t act, uint16_t* dX, void* dW,
+                                  int32_t dw_epilogue, int64_t M, int32_t F, int32_t K, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Step glue (stand-ins that close the denoising loop around the blocks; the
  * paper's sampler is DPM++ with default settings, whose coefficients it does not
  * give, so an Euler update x <- x + dsigma * v is used).

@@ -174,6 +174,11 @@ def _bind_ops(lib):
         "chorus_block_select": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, vp]),
         "chorus_attention_blocks_workspace_bytes": (sz, [i64, i32, i32, i32]),
         "chorus_attention_blocks": (i32, [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, i32, vp, sz, vp]),
+        "chorus_quant_rows_i8": (i32, [vp, i64, vp, vp, i64, i32, i32, vp]),
+        "chorus_gemm_i8": (i32, [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp]),
+        "chorus_gated_ffn": (i32, [vp, vp, i32, vp, vp, i64, i32, i32, vp]),
+        "chorus_gated_ffn_backward_workspace_bytes": (sz, [i64, i32, i32]),
+        "chorus_gated_ffn_backward": (i32, [vp, vp, vp, vp, i32, vp, vp, i32, i64, i32, i32, vp, sz, vp]),
         "chorus_glue_workspace_bytes": (sz, [i32, i32, i64]),
         "chorus_patch_embed": (i32, [vp, i32, i32, i32, i32, i32, i32, vp, i64, GW, i32, vp, vp, sz, vp]),
         "chorus_head_update": (i32, [vp, vp, i64, vp, GW, vp, f32, i32, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
@@ -635,6 +640,87 @@ def chorus_gemm_bf16_two_plan(M, N, M2, N2, K):
     kernel = C.c_int32(-1)
     _status("chorus_gemm_bf16_two_plan", load().chorus_gemm_bf16_two_plan(M, N, M2, N2, K, C.byref(kernel)))
     return kernel.value
+
+
+def chorus_quant_rows_i8(X, codes=None, scale=None):
+    """Rows of X (bf16 [M, K], rows any distance apart) to (int8 codes [M, Kp], fp32 scales [M]); Kp: K rounded up to 128, or that of `codes`."""
+    lib = load()
+    if X.dim() != 2 or X.stride(1) != 1:
+        raise TypeError("X: rows of neighbouring values required")
+    if not X.is_cuda or X.dtype != torch.bfloat16:
+        raise TypeError("X: device tensor of bfloat16 required")
+    M, K = X.shape
+    if codes is None:
+        codes = torch.empty(M, -(-K // 128) * 128, dtype=torch.int8, device=X.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=X.device)
+    _chk(codes, torch.int8, "codes")
+    _chk(scale, torch.float32, "scale", (M,))
+    if codes.dim() != 2 or codes.shape[0] != M:
+        raise TypeError("codes: wrong shape")
+    ld = X.stride(0) if M > 1 else max(K, X.stride(0))
+    _status("chorus_quant_rows_i8", lib.chorus_quant_rows_i8(_p(X), ld, _p(codes), _p(scale), M, K, codes.shape[1], _stream()))
+    return codes, scale
+
+
+def chorus_gemm_i8(A, a_scale, W, w_scale, epilogue, out, bias=None, gate0=None, gate1=None, scale=1.0):
+    """out = epilogue(A W^T, scaled by a_scale of the row and w_scale of the column, + bias); A [M, K], W [N, K] int8."""
+    lib = load()
+    _chk(A, torch.int8, "A")
+    _chk(W, torch.int8, "W")
+    (M, K), N = A.shape, W.shape[0]
+    if W.shape[1] != K:
+        raise TypeError("A/W inner dimensions differ")
+    _chk(a_scale, torch.float32, "a_scale", (M,))
+    _chk(w_scale, torch.float32, "w_scale", (N,))
+    _chk(out, torch.float32 if epilogue in (EPI_F32, EPI_RESID) else torch.bfloat16, "out", (M, N))
+    for n, t in (("bias", bias), ("gate0", gate0), ("gate1", gate1)):
+        _chk(t, torch.float32, n, (N,))
+    _status("chorus_gemm_i8", lib.chorus_gemm_i8(_p(A), _p(a_scale), _p(W), _p(w_scale), M, N, K, epilogue, _p(out), _p(bias), _p(gate0),
+                                                 _p(gate1), float(scale), _stream()))
+    return out
+
+
+ACT_GELU, ACT_SILU = 0, 1
+
+
+def chorus_gated_ffn(X, W, act, H, pre=None):
+    """H = act(X Wg^T) * (X Wu^T); W [2F, K] the rows of the gate, then of the other factor. pre [M, 2F]: both projections, for the backward pass."""
+    lib = load()
+    _chk(X, torch.bfloat16, "X")
+    _chk(W, torch.bfloat16, "W")
+    (M, K), F = X.shape, W.shape[0] // 2
+    if W.shape != (2 * F, K):
+        raise TypeError("X/W dimensions differ")
+    _chk(H, torch.bfloat16, "H", (M, F))
+    _chk(pre, torch.bfloat16, "pre", (M, 2 * F))
+    _status("chorus_gated_ffn", lib.chorus_gated_ffn(_p(X), _p(W), int(act), _p(H), _p(pre), M, F, K, _stream()))
+    return H
+
+
+def chorus_gated_ffn_backward_workspace_bytes(M, F, K) -> int:
+    return load().chorus_gated_ffn_backward_workspace_bytes(M, F, K)
+
+
+def chorus_gated_ffn_backward(X, W, pre, dH, act, dX, dW, accumulate=False, ws=None):
+    """dX and dW (either may be None) from dH and what the forward pass left in pre. dW bf16 or fp32; accumulate: fp32, added to dW."""
+    lib = load()
+    _chk(X, torch.bfloat16, "X")
+    _chk(W, torch.bfloat16, "W")
+    (M, K), F = X.shape, W.shape[0] // 2
+    if W.shape != (2 * F, K):
+        raise TypeError("X/W dimensions differ")
+    _chk(pre, torch.bfloat16, "pre", (M, 2 * F))
+    _chk(dH, torch.bfloat16, "dH", (M, F))
+    _chk(dX, torch.bfloat16, "dX", (M, K))
+    full = accumulate or (dW is not None and dW.dtype == torch.float32)
+    _chk(dW, torch.float32 if full else torch.bfloat16, "dW", (2 * F, K))
+    if ws is None:
+        ws = _ws(lib.chorus_gated_ffn_backward_workspace_bytes(M, F, K), X.device)
+    _status("chorus_gated_ffn_backward",
+            lib.chorus_gated_ffn_backward(_p(X), _p(W), _p(pre), _p(dH), int(act), _p(dX), _p(dW),
+                                          EPI_RESID if accumulate else EPI_F32 if full else EPI_BF16, M, F, K, _p(ws), ws.numel(), _stream()))
+    return dX, dW
 
 
 def chorus_ln_modulate(x, out, mul0, mul1, add0, add1, plus_one):

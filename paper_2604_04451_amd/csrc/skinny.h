@@ -1,0 +1,120 @@
+// Products of a few rows with large weight matrices, C = A W^T: what they take is the time to read the weights, once. A workgroup has a
+// strip of 16 rows of W (of both matrices with NB = 2) and all rows of A; its waves share out K, in pieces of 512 bytes (256 with two
+// matrices) of each row, and go on with what stands NW pieces further while the piece before is multiplied. Weights go from memory
+// straight into the registers that the matrix pipe reads: 16 rows of 64 bytes an instruction. Nothing is shared between workgroups
+// but A, which stays in the L2s; the waves' sums meet in LDS and are added in the order of the waves.
+#pragma once
+#include "gemm_tile.h"
+
+namespace chorus {
+
+constexpr int kSkinnyRows = 64;   // most rows of A: four blocks of 16
+constexpr int kSkinnyWaves = 8;   // most waves of a workgroup
+
+template <class MMA, int NB, int MB, class OUT>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_t* __restrict__ A, const uint16_t* __restrict__ W,
+                                                                   const uint16_t* __restrict__ W2, int M, int N, int K, OUT out) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef typename MMA::Acc Acc;
+  constexpr int U = NB == 2 || MB > 1 ? 2 : 4;  // groups of 64 units (128 bytes) of a row in a piece
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];
+  Acc* const part = reinterpret_cast<Acc*>(smem_raw);  // [waves][NB MB][64]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int lj = lane & 15, lg = lane >> 4;
+  const int n0 = 16 * xcd_remap(blockIdx.x, gridDim.x), row = n0 + lj < N ? n0 + lj : N - 1;
+  const uint16_t* w[NB];
+  w[0] = W + (size_t)row * K + 8 * lg;
+  if (NB == 2) w[NB - 1] = W2 + (size_t)row * K + 8 * lg;
+  const uint16_t* a[MB];
+  bool live[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb) {
+    live[mb] = 16 * mb + lj < M;
+    a[mb] = A + (size_t)(live[mb] ? 16 * mb + lj : 0) * K + 8 * lg;
+  }
+  const int groups = K / BK;
+  struct Piece {
+    bf16x8 w[U][2][NB], a[U][2][MB];
+  };
+  auto load = [&](Piece& p, int g) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = (g + u < groups ? g + u : groups - 1) * BK + 32 * h;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          p.w[u][h][nb] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w[nb] + at)));
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          p.a[u][h][mb] = bf16x8{};
+          if (live[mb] && g + u < groups) p.a[u][h][mb] = *reinterpret_cast<const bf16x8*>(a[mb] + at);
+        }
+      }
+  };
+  Acc acc[NB][MB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = Acc{};
+  const int step = waves * U;
+  Piece cur, next;
+  int g = wave * U;
+  if (g < groups) load(cur, g);
+  for (; g < groups; g += step) {
+    if (g + step < groups) load(next, g + step);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = MMA::mma(acc[nb][mb], cur.w[u][h][nb], cur.a[u][h][mb]);
+    cur = next;
+  }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) part[(wave * NB * MB + nb * MB + mb) * 64 + lane] = acc[nb][mb];
+  __syncthreads();
+  for (int mb = wave; mb < MB; mb += waves) {
+    Acc sum[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      sum[nb] = part[(nb * MB + mb) * 64 + lane];
+      for (int k = 1; k < waves; ++k) sum[nb] += part[(k * NB * MB + nb * MB + mb) * 64 + lane];
+    }
+    const int m = 16 * mb + lj, n = n0 + 4 * lg;
+    if (m < M && n < N) out(sum, (long)m, n);
+  }
+#endif
+}
+
+// Whether a product of M rows goes this way, N rows of all weight matrices, K in units of 2 bytes.
+inline bool skinny_rows(int64_t M, int64_t N, int32_t K) { return M <= 16; }
+
+// N = rows of each weight matrix, K in units of 2 bytes.
+template <class MMA, int NB, class OUT>
+int32_t launch_skinny(const uint16_t* A, const uint16_t* W, const uint16_t* W2, int M, int N, int K, const OUT& out, hipStream_t s) {
+  const int strips = (N + 15) / 16, groups = K / BK;
+  // waves for all units at once where the strips are few, as long as each has a piece
+  int waves = strips <= 1024 ? 8 : 4;
+  while (waves > 1 && waves * 2 > groups) waves /= 2;
+  const int blocks = (M + 15) / 16;
+#define SKINNY(MB)                                                                                                                       \
+  {                                                                                                                                      \
+    auto kern = skinny_kernel<MMA, NB, MB, OUT>;                                                                                         \
+    static DynLdsOnce once;                                                                                                              \
+    CHK_STATUS(once.ensure(reinterpret_cast<const void*>(kern), kSkinnyWaves* NB* MB * 1024));                                           \
+    hipLaunchKernelGGL(kern, dim3((unsigned)strips), dim3(64 * waves), (size_t)waves * NB * MB * 1024, s, A, W, W2, M, N, K, out);       \
+  }
+  if (blocks == 1) SKINNY(1)
+  else if (blocks == 2) SKINNY(2)
+  else SKINNY(4)
+#undef SKINNY
+  CHORUS_LAUNCH_CHECK();
+  return CHORUS_OK;
+}
+
+}  // namespace chorus
