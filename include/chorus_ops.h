@@ -247,6 +247,57 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
                        int32_t epilogue, void* out, const float* bias, const float* gate0, const float* gate1, float scale, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Attention with a learned bias by the distance between query and key, as text encoders (and decoders) have it, over a padded batch, and its
+ * gradients. Rows are read and written where projections leave and want them: value (b, row, head, i) of a tensor stands at
+ * b * batch + row * row_step + head * dh + i, so that queries, keys and values may lie side by side, or in a cache with room behind.
+ *   logit(i, j) = scale * q_i . k_j + table[bucket[clamp(d, -far, far) + far]][head],  d = j - (first[b] + i)
+ *   query i of sequence b sees the keys j < lens[b] (at most Lk), and with causal only those with d <= 0
+ *   O = softmax(logits) V; a row that sees no key, or only logits of -inf, is zeros. Keys and values behind lens[b] are not read.
+ *
+ * chorus_bias_attention
+ *   B, Lq, Lk, H, Hk, dh   sequences, queries and keys of each, heads, heads of keys and values (H % Hk == 0; head h reads h / (H / Hk)); dh in {64, 128}
+ *   n_buckets, far         rows of the table; distance from which on all share the bucket at the end, 0 to 1024
+ *   causal, scale          scale > 0, finite
+ *   *_row, *_batch         steps in values, multiples of 8; a row step at least heads * dh and at most 2^23
+ * chorus_bias_buckets: host only; the usual map: bucket host [2 far + 1], the buckets of distances -far .. far. One bucket each for the
+ *   nearest half of a side's buckets, near of them, then bucket near + k from the first n with (n / near)^(steps) >= (far / near)^k, steps the
+ *   other half. both_sides: the second half of all buckets is for keys ahead of the query (n_buckets even); otherwise those share bucket 0.
+ * chorus_attention_bias
+ *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
+ *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
+ *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass
+ *   rest        dev bf16 as O or NULL: what the rounding of O left off, for the backward pass
+ *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
+ *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe.
+ * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
+ *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
+ *   dtable dev fp32 [n_buckets, H]. steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
+ *   ws  dev, chorus_attention_bias_backward_workspace_bytes bytes; scratch of this call alone. Outputs must not overlap inputs. B, Lq or Lk of 0:
+ *   CHORUS_E_SHAPE (the forward pass accepts them).
+ * Limits: Lq, Lk up to 2^28, B up to 2^20, H up to 2^16, B * H * ceil(L / 128) up to 2^22 for L = Lq, Lk (CHORUS_E_SHAPE).
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int64_t Lq, Lk;
+  int32_t B, H, Hk, dh;
+  int32_t n_buckets, far, causal;
+  float scale;
+  int64_t q_row, q_batch, k_row, k_batch, v_row, v_batch, o_row, o_batch;
+} chorus_bias_attention;
+typedef struct {
+  int64_t do_row, do_batch, dq_row, dq_batch, dk_row, dk_batch, dv_row, dv_batch;
+} chorus_bias_attention_steps;
+int32_t chorus_bias_buckets(int32_t n_buckets, int32_t far, int32_t both_sides, int32_t* bucket);
+size_t chorus_attention_bias_workspace_bytes(const chorus_bias_attention* a);
+int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q, const uint16_t* K, const uint16_t* V, uint16_t* O, uint16_t* rest,
+                              float* lse, const float* table, const int32_t* bucket, const int32_t* lens, const int32_t* first, void* ws,
+                              size_t ws_bytes, void* stream);
+size_t chorus_attention_bias_backward_workspace_bytes(const chorus_bias_attention* a);
+int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const chorus_bias_attention_steps* steps, const uint16_t* Q, const uint16_t* K,
+                                       const uint16_t* V, const uint16_t* O, const uint16_t* rest, const float* lse, const uint16_t* dO,
+                                       const float* table, const int32_t* bucket, const int32_t* lens, const int32_t* first, uint16_t* dQ, uint16_t* dK,
+                                       uint16_t* dV, float* dtable, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * The gated half of a feed-forward block, as text encoders have it, and its gradients: h = act(x Wg^T) * (x Wu^T). The product with the
  * second matrix is chorus_gemm_bf16's.
  *   X   dev bf16 [M, K]

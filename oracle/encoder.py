@@ -115,13 +115,13 @@ def attention_bias_backward(q, k, v, table, bucket, lens, first, causal, scale, 
             dp = d @ v[b, :, g].T
             delta = (p * dp).sum(1, keepdims=True)
             ds = p * (dp - delta)
-            # what the products and the subtraction are made of, for the roundings of p and ds to 8 bits and of the sums to 24
+            # what the products and the subtraction are made of
             size = p * (np.abs(d) @ np.abs(v[b, :, g]).T + np.abs(d * o[b, :, h]).sum(1, keepdims=True))
             dq[b, :, h] = ds @ k[b, :, g] * scale
             dk[b, :, g] += ds.T @ q[b, :, h] * scale
             dv[b, :, g] += p.T @ d
             np.add.at(dtable[:, h], of.ravel(), ds.ravel())
-            a = np.abs(ds) + 2.0 ** -8 * size
+            a = np.abs(ds) + 2.0 ** -6 * size
             mq[b, :, h] = a @ np.abs(k[b, :, g]) * scale
             mk[b, :, g] += a.T @ np.abs(q[b, :, h]) * scale
             mv[b, :, g] += p.T @ np.abs(d)

@@ -88,6 +88,15 @@ class HierarchyPlan(C.Structure):
                 ("lds_bytes", C.c_int32)]
 
 
+class BiasAttention(C.Structure):
+    _fields_ = ([("Lq", C.c_int64), ("Lk", C.c_int64)] + [(n, C.c_int32) for n in ("B", "H", "Hk", "dh", "n_buckets", "far", "causal")] +
+                [("scale", C.c_float)] + [(n, C.c_int64) for n in ("q_row", "q_batch", "k_row", "k_batch", "v_row", "v_batch", "o_row", "o_batch")])
+
+
+class BiasAttentionSteps(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("do_row", "do_batch", "dq_row", "dq_batch", "dk_row", "dk_batch", "dv_row", "dv_batch")]
+
+
 class RunResult(C.Structure):
     _fields_ = [("index", C.c_int32), ("score", C.c_float), ("hit", C.c_int32), ("K1", C.c_int32),
                 ("K2", C.c_int32), ("Ls", C.c_int32)]
@@ -176,6 +185,11 @@ def _bind_ops(lib):
         "chorus_attention_blocks": (i32, [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, i32, vp, sz, vp]),
         "chorus_quant_rows_i8": (i32, [vp, i64, vp, vp, i64, i32, i32, vp]),
         "chorus_gemm_i8": (i32, [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp]),
+        "chorus_bias_buckets": (i32, [i32, i32, i32, C.POINTER(i32)]),
+        "chorus_attention_bias_workspace_bytes": (sz, [C.POINTER(BiasAttention)]),
+        "chorus_attention_bias": (i32, [C.POINTER(BiasAttention)] + [vp] * 11 + [sz, vp]),
+        "chorus_attention_bias_backward_workspace_bytes": (sz, [C.POINTER(BiasAttention)]),
+        "chorus_attention_bias_backward": (i32, [C.POINTER(BiasAttention), C.POINTER(BiasAttentionSteps)] + [vp] * 16 + [sz, vp]),
         "chorus_gated_ffn": (i32, [vp, vp, i32, vp, vp, i64, i32, i32, vp]),
         "chorus_gated_ffn_backward_workspace_bytes": (sz, [i64, i32, i32]),
         "chorus_gated_ffn_backward": (i32, [vp, vp, vp, vp, i32, vp, vp, i32, i64, i32, i32, vp, sz, vp]),
@@ -679,6 +693,84 @@ def chorus_gemm_i8(A, a_scale, W, w_scale, epilogue, out, bias=None, gate0=None,
     _status("chorus_gemm_i8", lib.chorus_gemm_i8(_p(A), _p(a_scale), _p(W), _p(w_scale), M, N, K, epilogue, _p(out), _p(bias), _p(gate0),
                                                  _p(gate1), float(scale), _stream()))
     return out
+
+
+def chorus_bias_buckets(n_buckets, far, both_sides=True, device="cuda"):
+    """int32 [2 far + 1]: the usual buckets of the distances -far .. far of a key from its query, on `device`."""
+    out = (C.c_int32 * (2 * max(int(far), 0) + 1))()
+    _status("chorus_bias_buckets", load().chorus_bias_buckets(int(n_buckets), int(far), int(bool(both_sides)), out))
+    return torch.tensor(list(out), dtype=torch.int32, device=device)
+
+
+def _heads(t, name, shape):
+    """(row step, batch step) of a bf16 tensor [B, L, heads, dh] whose heads lie one behind the other."""
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name}: device tensor of bfloat16 required")
+    if tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    batch, row, head, one = t.stride()
+    n, rows, heads, dh = shape
+    if one != 1 or (heads > 1 and head != dh):
+        raise TypeError(f"{name}: the heads of a row must lie one behind the other")
+    return row if rows > 1 else heads * dh, batch if n > 1 else 0
+
+
+def _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest):
+    if Q.dim() != 4 or K.dim() != 4 or V.dim() != 4 or O.dim() != 4:
+        raise TypeError("Q, K, V, O: [batch, rows, heads, dh] required")
+    B, Lq, H, dh = Q.shape
+    Lk, Hk = K.shape[1], K.shape[2]
+    a = BiasAttention(Lq, Lk, B, H, Hk, dh, table.shape[0], (bucket.numel() - 1) // 2, int(bool(causal)), float(scale),
+                      *_heads(Q, "Q", (B, Lq, H, dh)), *_heads(K, "K", (B, Lk, Hk, dh)), *_heads(V, "V", (B, Lk, Hk, dh)),
+                      *_heads(O, "O", (B, Lq, H, dh)))
+    _chk(table, torch.float32, "table", (table.shape[0], H))
+    _chk(bucket, torch.int32, "bucket", (2 * a.far + 1,))
+    _chk(lens, torch.int32, "lens", (B,))
+    _chk(first, torch.int32, "first", (B,))
+    _chk(lse, torch.float32, "lse", (B, H, Lq))
+    if rest is not None and _heads(rest, "rest", (B, Lq, H, dh)) != (a.o_row, a.o_batch):
+        raise TypeError("rest: must be laid out as O")
+    return a
+
+
+def chorus_attention_bias_workspace_bytes(a: BiasAttention) -> int:
+    return load().chorus_attention_bias_workspace_bytes(C.byref(a))
+
+
+def chorus_attention_bias(Q, K, V, O, table, bucket, lens=None, first=None, causal=False, scale=1.0, lse=None, rest=None, ws=None):
+    """O = softmax(scale Q K^T + table[bucket of the distance]) V. Q, O [B, Lq, H, dh], K, V [B, Lk, Hk, dh], rows any distance apart; lens int32 [B]:
+    keys of each sequence; first int32 [B]: position of query 0 among the keys; lse [B, H, Lq] and rest (as O) for the backward pass."""
+    lib = load()
+    a = _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest)
+    if ws is None:
+        need = lib.chorus_attention_bias_workspace_bytes(C.byref(a))
+        ws = _ws(need, Q.device) if need else None
+    _status("chorus_attention_bias", lib.chorus_attention_bias(C.byref(a), _p(Q), _p(K), _p(V), _p(O), _p(rest), _p(lse), _p(table), _p(bucket),
+                                                               _p(lens), _p(first), _p(ws), 0 if ws is None else ws.numel(), _stream()))
+    return O
+
+
+def chorus_attention_bias_backward_workspace_bytes(a: BiasAttention) -> int:
+    return load().chorus_attention_bias_backward_workspace_bytes(C.byref(a))
+
+
+def chorus_attention_bias_backward(Q, K, V, O, rest, lse, dO, table, bucket, dQ, dK, dV, dtable, lens=None, first=None, causal=False, scale=1.0,
+                                   ws=None):
+    """dQ, dK, dV (as Q, K, V, rows any distance apart) and dtable [n_buckets, H] fp32 from dO and what the forward pass left in O, rest and lse."""
+    lib = load()
+    a = _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest)
+    q, k = (a.B, a.Lq, a.H, a.dh), (a.B, a.Lk, a.Hk, a.dh)
+    for n, t in (("dO", dO), ("dQ", dQ), ("dK", dK), ("dV", dV)):
+        if t.dim() != 4:
+            raise TypeError(f"{n}: [batch, rows, heads, dh] required")
+    steps = BiasAttentionSteps(*_heads(dO, "dO", q), *_heads(dQ, "dQ", q), *_heads(dK, "dK", k), *_heads(dV, "dV", k))
+    _chk(dtable, torch.float32, "dtable", (a.n_buckets, a.H))
+    if ws is None:
+        ws = _ws(lib.chorus_attention_bias_backward_workspace_bytes(C.byref(a)), Q.device)
+    _status("chorus_attention_bias_backward",
+            lib.chorus_attention_bias_backward(C.byref(a), C.byref(steps), _p(Q), _p(K), _p(V), _p(O), _p(rest), _p(lse), _p(dO), _p(table),
+                                               _p(bucket), _p(lens), _p(first), _p(dQ), _p(dK), _p(dV), _p(dtable), _p(ws), ws.numel(), _stream()))
+    return dQ, dK, dV, dtable
 
 
 ACT_GELU, ACT_SILU = 0, 1

@@ -1,0 +1,150 @@
+// Attention with a learned bias by the distance between query and key: what its forward and backward kernels share.
+#pragma once
+#include "chorus_ops.h"
+#include "common.h"
+
+namespace chorus {
+
+constexpr int kTileKeys = 64;      // keys (or, where keys stand still, queries) of a step, in LDS
+constexpr int kTileQueries = 128;  // queries (or keys) of a workgroup: four waves of 32
+constexpr int kPad = 96;           // a near tile's distances reach 63 + 31 behind the farthest
+constexpr int kMostFar = 1024;
+constexpr int64_t kMostTokens = 1 << 28;
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A tensor of heads as the kernels see it: value (b, row, head, i) at p + b * batch + row * row_step + head * dh + i.
+struct Rows {
+  const uint16_t* p;
+  long row, batch;
+};
+struct RowsOut {
+  uint16_t* p;
+  long row, batch;
+};
+
+struct BiasArgs {
+  const float* table;     // [n_buckets, H]
+  const int* bucket;      // [2 far + 1]
+  const int* lens;        // [B] or null
+  const int* first;       // [B] or null
+  int n_buckets, far, causal;
+  float scale;
+  __device__ __forceinline__ int keys(int b, long Lk) const {
+    if (!lens) return (int)Lk;
+    const int n = lens[b];
+    return n < 0 ? 0 : n > (int)Lk ? (int)Lk : n;
+  }
+  __device__ __forceinline__ int origin(int b) const {  // position of query 0 among the keys
+    const int most = 1 << 29;
+    const int f = first ? first[b] : 0;
+    return f < -most ? -most : f > most ? most : f;
+  }
+  __host__ __device__ int width() const { return 2 * (far + kPad) + 1; }  // distances that a bias or a sum is kept for, the ends repeated
+  // bias of distance i - (far + kPad), in powers of two; a bucket outside the table has none. Finite ones end at +-2^126, so that the lowest value of
+  // the type stays finite here and the difference of two biases does as well.
+  __device__ __forceinline__ float bias(int i, int head, int H) const {
+    int at = i - kPad;
+    at = at < 0 ? 0 : at > 2 * far ? 2 * far : at;
+    const int c = bucket[at];
+    const float v = (unsigned)c < (unsigned)n_buckets ? table[(long)c * H + head] : 0.f;
+    return __builtin_fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2E, -0x1p126f), 0x1p126f) : v;
+  }
+};
+
+// A tile of rows in LDS: DH values a row, its 16-byte pieces at position piece ^ swizzle(row), such that 16 rows of a piece and its
+// neighbour, which a fragment of rows takes, meet all banks, and so do 8 rows of 32 bytes, which a fragment of columns takes.
+template <int DH>
+__device__ __forceinline__ int tile_swizzle(int row) {
+  return DH == 128 ? (row & 7) << 1 : (row >> 1 & 3) << 1;
+}
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short i16x4;
+
+__device__ __forceinline__ void* uniform(const void* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)), lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)u);
+  return reinterpret_cast<void*>(((uint64_t)hi << 32) | lo);
+}
+
+#if defined(__HIP_DEVICE_COMPILE__)  // buffer descriptors are types of the device compiler's alone
+// 64 rows of DH values on their way from global memory to LDS, through registers: a copy straight into LDS would make the compiler wait for
+// all of them ahead of every transposing read. Each thread fetches the 16 bytes that belong at its place of the tile. Rows behind the last are
+// the last one again: nothing behind it is read.
+template <int DH>
+struct TileStage {
+  static constexpr int kLoads = DH / 32, kPieces = DH / 8, kRows = 256 / kPieces;  // of a thread for a tile; of a row; of the workgroup's loads
+  int row, piece, row_bytes, to;
+  u32x4 v[kLoads];
+  __device__ __forceinline__ TileStage(int tid, long row_step) {
+    row = tid / kPieces;
+    piece = (tid % kPieces ^ tile_swizzle<DH>(row)) * 16;
+    row_bytes = (int)(row_step * 2);
+    to = tid * 8;
+  }
+  // the tile whose first row is at p, of which `rest` more rows exist
+  __device__ __forceinline__ void fetch(const uint16_t* p, int rest) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(uniform(p), 0, -1, 0x00027000);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row + i * kRows;
+      v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (r < rest ? r : rest) * row_bytes + piece, 0, 0));
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* tile) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(tile + to + i * 2048) = v[i];
+  }
+};
+#endif
+
+// 16 rows of a tile as an operand of v_mfma_f32_16x16x32_bf16: lane l has row l % 16, values 32 kc + 8 (l / 16) .. + 8
+template <int DH>
+struct RowFragments {
+  int at[DH / 32];
+  __device__ __forceinline__ explicit RowFragments(int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int kc = 0; kc < DH / 32; ++kc) at[kc] = r * DH + ((4 * kc + g) ^ tile_swizzle<DH>(r)) * 8;
+  }
+  __device__ __forceinline__ bf16x8 read(const uint16_t* tile, int block, int kc) const {
+    return *reinterpret_cast<const bf16x8*>(tile + block * 16 * DH + at[kc]);
+  }
+};
+// 16 columns of 32 rows: lane l has column 16 db + l % 16, of rows 32 c + 4 (l / 16) + {0..3} and 16 further. One instruction takes 4 rows of 32 bytes
+// for 16 lanes, lane i of them 8 bytes from row i / 4, and hands lane i column i.
+template <int DH>
+struct ColumnFragments {
+  int at[DH / 16];
+  __device__ __forceinline__ explicit ColumnFragments(int lane) {
+    const int j = lane & 15, r = 4 * (lane >> 4) + (j >> 2);
+#pragma unroll
+    for (int db = 0; db < DH / 16; ++db) at[db] = r * DH + ((2 * db + (j >> 1 & 1)) ^ tile_swizzle<DH>(r)) * 8 + (j & 1) * 4;
+  }
+  __device__ __forceinline__ bf16x8 read(const uint16_t* tile, int c, int db) const {
+    typedef __attribute__((address_space(3))) i16x4* Lds4;
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(tile + 32 * c * DH + at[db]));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(tile + (32 * c + 16) * DH + at[db]));
+    bf16x8 v;
+    const bf16x4 a = __builtin_bit_cast(bf16x4, lo), b = __builtin_bit_cast(bf16x4, hi);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = a[e];
+      v[4 + e] = b[e];
+    }
+    return v;
+  }
+};
+
+__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float lane_value(int src, float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)__float_as_uint(v)));
+}
+
+bool bias_step_ok(int64_t row, int64_t batch, int64_t heads, int32_t dh);
+int32_t check_bias_sizes(const chorus_bias_attention* a);
+// The checks that both directions share; sets the kernels' view.
+int32_t check_bias_attention(const chorus_bias_attention* a, const float* table, const int32_t* bucket, const int32_t* lens, const int32_t* first,
+                             BiasArgs* out);
+
+}  // namespace chorus

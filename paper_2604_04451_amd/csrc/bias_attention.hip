@@ -1,0 +1,463 @@
+// Attention whose logits get a learned bias by the bucket of the distance between query and key, forward: O = softmax(scale Q K^T + bias) V, over
+// the keys of each sequence of a padded batch, causal or not, one query or many.
+//
+// The tiled kernel: a workgroup of four waves takes 128 queries of a head, 32 a wave in registers, and walks over the keys 64 at a time, in
+// tiles in LDS that come from the rows as a projection leaves them. S^T = K Q^T leaves a lane with the logits of one query
+// row in the order in which its weights are the operand of O^T += V^T P^T; V^T comes out of the rows of V by transposing LDS reads. The
+// step has the two phases of the kernels over whole and listed keys: the weights on the vector pipe; then this tile's share of the result and the
+// next one's logits on the matrix pipe, the next tiles on their way in registers meanwhile. One barrier a step.
+// The bias of a distance is in LDS, in powers of two, `far` and a tile's width to either side. A wave's 32 x 64 logits read it only where
+// some distance is below `far`; tiles beyond have one value, which joins the row's reference at no cost.
+#include "bias_attention.h"
+
+namespace chorus {
+namespace {
+
+constexpr int kMostSlices = 64;  // the join holds a slice a lane
+
+// Tiles of 128 queries whose workgroups leave compute units idle are cut into slices of the keys: about two workgroups for every unit, none of less
+// than four steps.
+int slices_of(long tiles, long Lk) {
+  const long steps = (Lk + kTileKeys - 1) / kTileKeys;
+  long s = tiles >= 256 ? 1 : (512 + tiles - 1) / tiles;
+  if (s > steps / 4) s = steps / 4;
+  return s < 1 ? 1 : s > kMostSlices ? kMostSlices : (int)s;
+}
+size_t slice_bytes(long tiles, int slices, int dh, int rows) {
+  return slices > 1 ? (size_t)tiles * slices * rows * (dh * sizeof(float) + sizeof(float2)) : 0;
+}
+
+struct Outputs {
+  RowsOut o;
+  uint16_t* rest;  // as o
+  float* lse;      // [B, H, Lq]
+};
+
+// SPLIT: for the backward pass, whose sums of gradients by bucket cancel to a small part of their terms, a weight's rounding is made up for by a
+// second product with what it left off (16 bits of a weight altogether), and so is that of the result by a second output.
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
+                                                                long Lk, int H, int group, int nq, int slices) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the buffer descriptors below are types of the device compiler's alone
+  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2;
+  constexpr int TILE = kTileKeys * DH;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values, biases
+  float* const s_bias = reinterpret_cast<float*>(smem + 4 * TILE);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 15, g = lane >> 4;
+  const int unit = xcd_remap(blockIdx.x, gridDim.x);
+  const int tile = unit / slices, slice = unit - tile * slices;
+  const int bh = tile / nq, qb = tile - bh * nq, b = bh / H, head = bh - b * H;
+  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int q0 = qb * kTileQueries + wave * 32;  // the wave's first query
+  const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
+  int most = n;  // keys that some query of the workgroup sees
+  if (bias.causal) {
+    const int m = origin + last_q + 1;
+    most = m < 0 ? 0 : m < n ? m : n;
+  }
+  const int steps = (most + kTileKeys - 1) / kTileKeys;
+  const int t0 = (int)((long)steps * slice / slices), t1 = (int)((long)steps * (slice + 1) / slices);
+
+  TileStage<DH> k_in(tid, K.row), v_in(tid, V.row);
+  const uint16_t* const k_base = K.p + (long)b * K.batch + (long)(head / group) * DH;
+  const uint16_t* const v_base = V.p + (long)b * V.batch + (long)(head / group) * DH;
+  auto fetch_k = [&](int t) { k_in.fetch(k_base + (long)t * kTileKeys * K.row, n - 1 - t * kTileKeys); };
+  auto fetch_v = [&](int t) { v_in.fetch(v_base + (long)t * kTileKeys * V.row, n - 1 - t * kTileKeys); };
+  if (t0 < t1) {
+    fetch_k(t0);
+    fetch_v(t0);
+  }
+  const int width = bias.width(), far = bias.far;
+  for (int i = tid; i < width; i += 256) s_bias[i] = bias.bias(i, head, H);
+
+  const RowFragments<DH> k_at(lane);
+  const ColumnFragments<DH> v_at(lane);
+  bf16x8 qf[RB][KC];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    long q = q0 + 16 * rb + lq;
+    if (q > Lq - 1) q = Lq - 1;
+    const uint16_t* qp = Q.p + (long)b * Q.batch + q * Q.row + (long)head * DH + 8 * g;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
+  }
+  if (t0 < t1) {
+    k_in.store(smem);
+    v_in.store(smem + 2 * TILE);
+    if (t0 + 1 < t1) fetch_k(t0 + 1);
+  }
+  f32x4 o[DB][RB], s[KB][RB];
+  // a row's reference, in powers of two, and its lane's share of the sum of its weights
+  float m_run[RB], l_run[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m_run[rb] = 0.f;
+    l_run[rb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bool fresh = true;       // some row of the wave has seen no finite logit
+  bool seen[RB] = {false, false};
+  const float scale = bias.scale * kLog2E;
+
+  lds_barrier();
+  const float below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
+  const float above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
+  if (t0 < t1) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        s[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) s[kb][rb] = mfma(k_at.read(smem, kb, kc), qf[rb][kc], s[kb][rb]);
+      }
+  }
+  if (t0 + 1 < t1) {
+    k_in.store(smem + TILE);
+    fetch_v(t0 + 1);
+    if (t0 + 2 < t1) fetch_k(t0 + 2);
+  }
+  lds_barrier();
+
+  // logits of tile t: scaled, with their bias, less the reference
+  auto logits = [&](int t) {
+    const int nearest = t * kTileKeys - (origin + q0);  // distance of the tile's first key from the wave's first query
+    if (nearest + 63 > -far && nearest - 31 < far) {
+      const float* at = s_bias + (nearest + far + kPad + 4 * g - lq);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, at[16 * (kb - rb) + i] - m_run[rb]);
+    } else {
+      const float c = nearest > 0 ? above : below;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, c - m_run[rb]);
+    }
+    int end = n;  // first key that the wave's first query does not see
+    if (bias.causal && origin + q0 + 1 < end) end = origin + q0 + 1;
+    if ((t + 1) * kTileKeys > end) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        int rest = n;
+        if (bias.causal && origin + q0 + 16 * rb + lq + 1 < n) rest = origin + q0 + 16 * rb + lq + 1;
+        rest -= t * kTileKeys + 4 * g;
+        asm volatile("" : "+v"(rest));  // compared here: hoisted, the results would fill the scalar registers
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * kb + i >= rest) s[kb][rb][i] = -INFINITY;
+      }
+    }
+  };
+  // The reference moves when a row exceeds it by more than 2^8, and to the first finite logit of a row whatever that is.
+  auto move = [&]() {
+    float mx[RB];
+    bool far_up = fresh;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      mx[rb] = s[0][rb][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[rb] = fmaxf(mx[rb], s[kb][rb][i]);
+      far_up = far_up || mx[rb] > 8.0f;
+    }
+    if (!__any(far_up)) return;
+    bool none = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float m = fmaxf(mx[rb], swap_rows16(mx[rb]));
+      m = fmaxf(m, swap_halves(m));
+      const bool finite = m > -INFINITY;
+      const float delta = !seen[rb] ? (finite ? m : 0.f) : fmaxf(m, 0.f);
+      const float alpha = !seen[rb] ? 1.0f : __builtin_amdgcn_exp2f(-delta);
+      seen[rb] = seen[rb] || finite;
+      none = none || !seen[rb];
+      m_run[rb] += delta;
+      l_run[rb] *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db][rb] *= alpha;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb][rb] -= delta;
+    }
+    fresh = __any(none);
+  };
+
+  int buf = 0;
+  for (int t = t0; t < t1; ++t, buf ^= 1) {
+    // ================= vector phase: the weights of this tile =================
+    __builtin_amdgcn_sched_barrier(0);
+    logits(t);
+    move();
+    bf16x8 pf[NC][RB], pl[NC][RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
+          l_run[rb] += p;
+          pf[c][rb][e] = (bf16_t)p;
+          if (SPLIT) pl[c][rb][e] = (bf16_t)(p - (float)pf[c][rb][e]);
+        }
+      }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        asm volatile("" : "+v"(pf[c][rb]));  // here and not where they are used
+        if (SPLIT) asm volatile("" : "+v"(pl[c][rb]));
+      }
+    // what was requested a step ago: the keys behind the next tile's over this tile's, whose logits are made, the next tile's values
+    // beside this one's
+    if (t + 2 < t1) k_in.store(smem + buf * TILE);
+    if (t + 1 < t1) v_in.store(smem + (2 + (buf ^ 1)) * TILE);
+    if (t + 3 < t1) fetch_k(t + 3);
+    if (t + 2 < t1) fetch_v(t + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    // ================= matrix phase: this tile's share of the result, and the logits of the next one =================
+    // A slot is two MFMAs and the read of the fragment that is used kAhead slots on.
+    __builtin_amdgcn_s_setprio(1);
+    constexpr int VS = DB * NC, SLOTS = VS + KB * KC, kAhead = 4;
+    bf16x8 fr[SLOTS];
+    auto read = [&](int f) {
+      fr[f] = f < VS ? v_at.read(smem + (2 + buf) * TILE, f % NC, f / NC) : k_at.read(smem + (buf ^ 1) * TILE, (f - VS) / KC, (f - VS) % KC);
+    };
+#pragma unroll
+    for (int f = 0; f < kAhead; ++f) read(f);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (i < VS) {
+          const int db = i / NC, rb = i % NC, c = u;
+          o[db][rb] = mfma(fr[db * NC + c], pf[c][rb], o[db][rb]);
+          if (SPLIT) o[db][rb] = mfma(fr[db * NC + c], pl[c][rb], o[db][rb]);
+        } else {
+          const int kb = (i - VS) / KC, at = (i - VS) % KC * 2 + u, rb = at / KC, kc = at % KC;
+          if (kc == 0) s[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+          s[kb][rb] = mfma(fr[VS + kb * KC + kc], qf[rb][kc], s[kb][rb]);
+        }
+      }
+      if (i + kAhead < SLOTS) read(i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    static_assert(NC == 2 && RB == 2 && SLOTS > kAhead, "a slot's two MFMAs");
+    __builtin_amdgcn_s_setprio(0);
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // On the way out four neighbouring lanes write 64 bytes of a row: they get them from the lanes of that row.
+  const auto from_lane = [](int src, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)v); };
+  const int row0 = q0 + (lq & 12) + g, b4 = lq & 3;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    l_run[rb] += swap_rows16(l_run[rb]);
+    l_run[rb] += swap_halves(l_run[rb]);
+    const float l = l_run[rb], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
+    const long row = row0 + 16 * rb, mine = q0 + 16 * rb + lq;
+    const bool live = row < Lq;
+    if (slices > 1) {
+      const long at = (long)unit * kTileQueries;
+      float* op = part + (at + (row - (long)qb * kTileQueries)) * DH + 4 * b4;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(from_lane(16 * b4 + (lq & 12) + g, __float_as_uint(o[db][rb][e])));
+        if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
+      }
+      if (g == 0 && mine < Lq)
+        reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - (long)qb * kTileQueries)] = make_float2(m_run[rb], l);
+      continue;
+    }
+    const long to = (long)b * out.o.batch + row * out.o.row + (long)head * DH + 8 * b4;
+    const int src = 16 * (b4 >> 1 | (b4 & 1) << 1) + (lq & 12) + g;
+    auto put = [&](uint16_t* p, bool rest) {
+#pragma unroll
+      for (int i = 0; i < DB / 2; ++i) {
+        // 4 values of block 2i and 4 of 2i + 1 here, and as many with the lane 16 further: after the swap eight of the one here, of
+        // the other there
+        f32x4 x = o[2 * i][rb] * inv, y = o[2 * i + 1][rb] * inv;
+        if (SPLIT && rest) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] -= bf16_to_f32(f32_to_bf16(x[e]));
+            y[e] -= bf16_to_f32(f32_to_bf16(y[e]));
+          }
+        }
+        const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[0], x[1]), pack_bf16x2(y[0], y[1]), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[2], x[3]), pack_bf16x2(y[2], y[3]), false, false);
+        const u32x4 v = {from_lane(src, lo[0]), from_lane(src, hi[0]), from_lane(src, lo[1]), from_lane(src, hi[1])};
+        if (live) *reinterpret_cast<u32x4*>(p + to + 32 * i) = v;
+      }
+    };
+    put(out.o.p, false);
+    if (SPLIT) put(out.rest, true);
+    if (out.lse && g == 0 && mine < Lq) out.lse[(long)bh * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
+  }
+#endif
+}
+
+// Puts the slices of a row together, a wave a row: the largest reference, then the slices' results and sums by their distance from it, in
+// an order that depends on nothing but their number.
+template <int DH>
+__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, Outputs out, long Lq, int H, int nq, int rows, int slices,
+                                                        long units) {
+  constexpr int E = DH / 64;  // values of a lane
+  const int lane = threadIdx.x & 63;
+  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long tile = at / rows;
+  const int row = (int)(at - tile * rows);
+  const long bh = tile / nq, q = (tile - bh * nq) * rows + row;
+  if (tile >= units / slices || q >= Lq) return;
+  const long first = tile * slices * rows + row;
+  const float2 ml = lane < slices ? reinterpret_cast<const float2*>(part + units * rows * DH)[first + (long)lane * rows] : make_float2(0.f, 0.f);
+  const float top = wave_max(ml.y != 0.f ? ml.x : -INFINITY);  // a slice without a key has no reference
+  const float w = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+  const float total = wave_sum(w * ml.y), inv = total == 0.f ? 0.f : 1.0f / total;
+  float sum[E] = {};
+  for (int s = 0; s < slices; ++s) {
+    const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+    const float* p = part + (first + (long)s * rows) * DH + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(ws, p[e], sum[e]);
+  }
+  const long b = bh / H, head = bh - b * H, to = b * out.o.batch + q * out.o.row + head * DH + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float v = sum[e] * inv;
+    const uint16_t r = f32_to_bf16(v);
+    out.o.p[to + e] = r;
+    if (out.rest) out.rest[to + e] = f32_to_bf16(v - bf16_to_f32(r));
+  }
+  if (out.lse && lane == 0) out.lse[bh * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+}
+
+struct ForwardPlan {
+  long tiles;
+  int nq, slices;
+  size_t bytes;
+};
+ForwardPlan forward_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dh) {
+  ForwardPlan p;
+  p.nq = (int)((Lq + kTileQueries - 1) / kTileQueries);
+  p.tiles = (long)(B * H * p.nq);
+  p.slices = slices_of(p.tiles, (long)Lk);
+  p.bytes = slice_bytes(p.tiles, p.slices, dh, kTileQueries);
+  return p;
+}
+constexpr int64_t kMostTiles = 1 << 22;
+
+}  // namespace
+
+bool bias_step_ok(int64_t row, int64_t batch, int64_t heads, int32_t dh) {
+  return row >= heads * dh && row <= (1 << 23) && row % 8 == 0 && batch >= 0 && batch % 8 == 0;
+}
+
+int32_t check_bias_sizes(const chorus_bias_attention* a) {
+  if (!a) return CHORUS_E_ARG;
+  if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->H <= 0 || a->Hk <= 0 || a->n_buckets <= 0 || a->far < 0) return CHORUS_E_ARG;
+  if (!(a->scale > 0.f) || a->scale > 3e38f) return CHORUS_E_ARG;
+  if ((a->dh != 64 && a->dh != 128) || a->H % a->Hk || a->far > kMostFar || a->Lq > kMostTokens || a->Lk > kMostTokens) return CHORUS_E_SHAPE;
+  if (a->H > (1 << 16) || a->B > (1 << 20)) return CHORUS_E_SHAPE;
+  if (!bias_step_ok(a->q_row, a->q_batch, a->H, a->dh) || !bias_step_ok(a->k_row, a->k_batch, a->Hk, a->dh) || !bias_step_ok(a->v_row, a->v_batch, a->Hk, a->dh) ||
+      !bias_step_ok(a->o_row, a->o_batch, a->H, a->dh))
+    return CHORUS_E_SHAPE;
+  const int64_t nq = (a->Lq + kTileQueries - 1) / kTileQueries, nk = (a->Lk + kTileQueries - 1) / kTileQueries;
+  if (nq * a->H > kMostTiles || nk * a->H > kMostTiles || nq * a->H * a->B > kMostTiles || nk * a->H * a->B > kMostTiles) return CHORUS_E_SHAPE;
+  return CHORUS_OK;
+}
+
+int32_t check_bias_attention(const chorus_bias_attention* a, const float* table, const int32_t* bucket, const int32_t* lens, const int32_t* first,
+                             BiasArgs* out) {
+  CHK_STATUS(check_bias_sizes(a));
+  if (a->B == 0 || a->Lq == 0) return CHORUS_OK;
+  if (!table || !bucket || !aligned16(table) || !aligned16(bucket) || !aligned16(lens) || !aligned16(first)) return CHORUS_E_ARG;
+  *out = BiasArgs{table, bucket, lens, first, a->n_buckets, a->far, a->causal != 0, a->scale};
+  return CHORUS_OK;
+}
+
+}  // namespace chorus
+
+using namespace chorus;
+
+extern "C" {
+
+// Steps of the logarithm by the condition (n / near)^steps >= (far / near)^k, whose two sides are the same number only where both are powers of
+// one root; long double keeps them to 10^-17 of their size, and two that differ are further apart for every far that the call takes.
+int32_t chorus_bias_buckets(int32_t n_buckets, int32_t far, int32_t both_sides, int32_t* bucket) {
+  const int side = both_sides ? n_buckets / 2 : n_buckets, near = side / 2, steps = side - near;
+  if (n_buckets < 2 || !bucket || (both_sides && n_buckets % 2) || near < 1) return CHORUS_E_ARG;
+  if (far > kMostFar || far <= near) return CHORUS_E_SHAPE;
+  for (int d = -far; d <= far; ++d) {
+    const int n = both_sides ? (d < 0 ? -d : d) : (d < 0 ? -d : 0);
+    int of = n;
+    if (n >= near) {
+      const long double at = (long double)steps * __builtin_logl((long double)n / near) / __builtin_logl((long double)far / near);
+      int k = (int)(at + 1e-12L);
+      of = near + (k < steps - 1 ? k : steps - 1);
+    }
+    bucket[d + far] = of + (both_sides && d > 0 ? side : 0);
+  }
+  return CHORUS_OK;
+}
+
+size_t chorus_attention_bias_workspace_bytes(const chorus_bias_attention* a) {
+  if (check_bias_sizes(a) != CHORUS_OK || a->B == 0 || a->Lq == 0) return 0;
+  return forward_plan(a->B, a->H, a->Lq, a->Lk, a->dh).bytes;
+}
+
+int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q, const uint16_t* K, const uint16_t* V, uint16_t* O, uint16_t* rest,
+                              float* lse, const float* table, const int32_t* bucket, const int32_t* lens, const int32_t* first, void* ws,
+                              size_t ws_bytes, void* stream) {
+  BiasArgs bias;
+  CHK_STATUS(check_bias_attention(a, table, bucket, lens, first, &bias));
+  if (a->B == 0 || a->Lq == 0) return CHORUS_OK;
+  if (!Q || !O || (a->Lk > 0 && (!K || !V))) return CHORUS_E_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(rest) || !aligned16(lse) || !aligned16(ws)) return CHORUS_E_ARG;
+  const ForwardPlan p = forward_plan(a->B, a->H, a->Lq, a->Lk, a->dh);
+  if (p.bytes && (!ws || ws_bytes < p.bytes)) return CHORUS_E_WORKSPACE;
+  const Rows q{Q, (long)a->q_row, (long)a->q_batch}, k{K, (long)a->k_row, (long)a->k_batch}, v{V, (long)a->v_row, (long)a->v_batch};
+  const Outputs out{RowsOut{O, (long)a->o_row, (long)a->o_batch}, rest, lse};
+  const long units = p.tiles * p.slices;
+  const int lds = 4 * kTileKeys * a->dh * 2 + bias.width() * 4, most = 4 * kTileKeys * a->dh * 2 + (2 * (kMostFar + kPad) + 1) * 4;
+  hipStream_t s = (hipStream_t)stream;
+#define ATTEND(DH, SPLIT)                                                                                                               \
+  do {                                                                                                                                  \
+    static DynLdsOnce once;                                                                                                             \
+    CHK_STATUS(once.ensure((const void*)bias_attention_kernel<DH, SPLIT>, most));                                                              \
+    hipLaunchKernelGGL((bias_attention_kernel<DH, SPLIT>), dim3((unsigned)units), dim3(256), lds, s, q, k, v, out, bias, (float*)ws,           \
+                       (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, p.nq, p.slices);                                                   \
+    CHORUS_LAUNCH_CHECK();                                                                                                              \
+    if (p.slices > 1) {                                                                                                                 \
+      hipLaunchKernelGGL((bias_join_kernel<DH>), dim3((unsigned)((p.tiles * kTileQueries + 3) / 4)), dim3(256), 0, s, (const float*)ws, \
+                         out, (long)a->Lq, a->H, p.nq, kTileQueries, p.slices, units);                                                  \
+      CHORUS_LAUNCH_CHECK();                                                                                                            \
+    }                                                                                                                                   \
+  } while (0)
+  if (a->dh == 128) {
+    if (rest) ATTEND(128, true);
+    else ATTEND(128, false);
+  } else {
+    if (rest) ATTEND(64, true);
+    else ATTEND(64, false);
+  }
+#undef ATTEND
+  return CHORUS_OK;
+}
+
+}  // extern "C"

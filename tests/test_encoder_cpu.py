@@ -66,6 +66,86 @@ def test_gated_backward_refuses(change, want):
     assert _gated_back(P.load(), **change) == want
 
 
+def _bias(**change):
+    a = B.BiasAttention(40, 50, 2, 4, 2, 64, 32, 128, 0, 1.0, 256, 40 * 256, 128, 50 * 128, 128, 50 * 128, 256, 40 * 256)
+    for n, v in change.items():
+        setattr(a, n, v)
+    return a
+
+
+def _attend(lib, a, Q=P16, K=P16, V=P16, O=P16, rest=NULL, lse=NULL, table=P16, bucket=P16, lens=NULL, first=NULL, ws=NULL, ws_bytes=0):
+    return lib.chorus_attention_bias(C.byref(a) if a is not None else None, Q, K, V, O, rest, lse, table, bucket, lens, first, ws, ws_bytes, NULL)
+
+
+SHAPES = [(dict(B=-1), B.E_ARG), (dict(Lq=-1), B.E_ARG), (dict(Lk=-1), B.E_ARG), (dict(H=0), B.E_ARG), (dict(Hk=0), B.E_ARG), (dict(n_buckets=0), B.E_ARG),
+          (dict(far=-1), B.E_ARG), (dict(scale=0.0), B.E_ARG), (dict(scale=-1.0), B.E_ARG), (dict(scale=float("nan")), B.E_ARG),
+          (dict(scale=float("inf")), B.E_ARG), (dict(dh=96), B.E_SHAPE), (dict(dh=32), B.E_SHAPE), (dict(Hk=3), B.E_SHAPE), (dict(far=1025), B.E_SHAPE),
+          (dict(Lq=(1 << 28) + 1), B.E_SHAPE), (dict(Lk=(1 << 28) + 1), B.E_SHAPE), (dict(q_row=248), B.E_SHAPE), (dict(k_row=120), B.E_SHAPE),
+          (dict(v_row=132), B.E_SHAPE), (dict(o_row=(1 << 23) + 8), B.E_SHAPE), (dict(q_batch=4), B.E_SHAPE), (dict(k_batch=-8), B.E_SHAPE),
+          (dict(B=1 << 20, Lq=1 << 12), B.E_SHAPE), (dict(B=1 << 20, Lk=1 << 12), B.E_SHAPE), (dict(H=1 << 17, q_row=1 << 23, o_row=1 << 23), B.E_SHAPE)]
+
+
+@pytest.mark.parametrize("change,want", SHAPES + [(dict(B=0), B.OK), (dict(Lq=0), B.OK)])
+def test_attention_bias_refuses_shapes(change, want):
+    assert _attend(P.load(), _bias(**change)) == want
+
+
+@pytest.mark.parametrize("change,want", [(dict(Q=NULL), B.E_ARG), (dict(K=NULL), B.E_ARG), (dict(V=NULL), B.E_ARG), (dict(O=NULL), B.E_ARG),
+                                         (dict(table=NULL), B.E_ARG), (dict(bucket=NULL), B.E_ARG), (dict(Q=P8), B.E_ARG), (dict(K=P8), B.E_ARG),
+                                         (dict(V=P8), B.E_ARG), (dict(O=P8), B.E_ARG), (dict(rest=P8), B.E_ARG), (dict(lse=P8), B.E_ARG),
+                                         (dict(table=P8), B.E_ARG), (dict(bucket=P8), B.E_ARG), (dict(lens=P8), B.E_ARG), (dict(first=P8), B.E_ARG),
+                                         (dict(ws=P8), B.E_ARG)])
+def test_attention_bias_refuses_pointers(change, want):
+    assert _attend(P.load(), _bias(), **change) == want
+    assert _attend(P.load(), None) == B.E_ARG
+
+
+def test_attention_bias_workspace():
+    lib = P.load()
+    size = lib.chorus_attention_bias_workspace_bytes
+    few = _bias(Lk=4096, Lq=40)
+    assert size(C.byref(few)) > 0 and size(C.byref(_bias(B=1024))) == 0 and size(C.byref(_bias(dh=96))) == 0 and size(None) == 0
+    assert _attend(lib, few, ws=P16, ws_bytes=size(C.byref(few)) - 1) == B.E_WORKSPACE and _attend(lib, few) == B.E_WORKSPACE
+
+
+STEPS = dict(do_row=256, do_batch=10240, dq_row=256, dq_batch=10240, dk_row=128, dk_batch=6400, dv_row=128, dv_batch=6400)
+
+
+def _attend_back(lib, a, steps=None, Q=P16, K=P16, V=P16, O=P16, rest=P16, lse=P16, dO=P16, table=P16, bucket=P16, lens=NULL, first=NULL, dQ=P16, dK=P16,
+                 dV=P16, dtable=P16, ws=P16, ws_bytes=1 << 40):
+    st = B.BiasAttentionSteps(**{**STEPS, **(steps or {})})
+    return lib.chorus_attention_bias_backward(C.byref(a), C.byref(st), Q, K, V, O, rest, lse, dO, table, bucket, lens, first, dQ, dK, dV, dtable, ws,
+                                              ws_bytes, NULL)
+
+
+@pytest.mark.parametrize("change,want", SHAPES + [(dict(B=0), B.E_SHAPE), (dict(Lq=0), B.E_SHAPE), (dict(Lk=0), B.E_SHAPE)])
+def test_attention_bias_backward_refuses_shapes(change, want):
+    assert _attend_back(P.load(), _bias(**change)) == want
+
+
+@pytest.mark.parametrize("change,want", [(dict([(n, v)]), B.E_ARG) for n in ("Q", "K", "V", "O", "rest", "lse", "dO", "table", "bucket", "dQ", "dK", "dV",
+                                                                              "dtable") for v in (NULL, P8)] +
+                         [(dict(lens=P8), B.E_ARG), (dict(first=P8), B.E_ARG), (dict(ws=P8), B.E_ARG), (dict(ws=NULL), B.E_WORKSPACE),
+                          (dict(ws_bytes=1000), B.E_WORKSPACE), (dict(steps=dict(do_row=248)), B.E_SHAPE), (dict(steps=dict(dq_batch=4)), B.E_SHAPE),
+                          (dict(steps=dict(dk_row=1 << 24)), B.E_SHAPE), (dict(steps=dict(dv_batch=-8)), B.E_SHAPE)])
+def test_attention_bias_backward_refuses_pointers(change, want):
+    assert _attend_back(P.load(), _bias(), **change) == want
+
+
+@pytest.mark.parametrize("n,far,both", [(32, 128, 1), (32, 128, 0), (8, 8, 0), (64, 512, 1), (16, 1024, 1), (12, 100, 1), (2, 7, 0), (4, 3, 1), (20, 11, 1)])
+def test_bias_buckets(n, far, both):
+    out = (C.c_int32 * (2 * far + 1))()
+    assert P.load().chorus_bias_buckets(n, far, both, out) == B.OK
+    assert list(out) == OE.bias_buckets(n, far, bool(both)).tolist()
+
+
+def test_bias_buckets_refuses():
+    lib, out = P.load(), (C.c_int32 * 4096)()
+    for n, far, both, to, want in ((1, 8, 0, out, B.E_ARG), (2, 8, 1, out, B.E_ARG), (33, 128, 1, out, B.E_ARG), (0, 8, 0, out, B.E_ARG),
+                                   (32, 128, 1, None, B.E_ARG), (32, 1025, 1, out, B.E_SHAPE), (32, 8, 1, out, B.E_SHAPE), (32, -1, 0, out, B.E_SHAPE)):
+        assert lib.chorus_bias_buckets(n, far, both, to) == want, (n, far, both)
+
+
 def test_gated_backward_workspace():
     size = P.load().chorus_gated_ffn_backward_workspace_bytes
     M, F, K = 100, 128, 64
