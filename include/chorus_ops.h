@@ -266,9 +266,10 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
  *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
  *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass
- *   rest        dev bf16 as O or NULL: what the rounding of O left off, for the backward pass
+ *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass (whose
+ *               sums by bucket cancel to a small part of their terms). With it the weights count with 24 bits.
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
- *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe.
+ *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe (without rest).
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
  *   dtable dev fp32 [n_buckets, H]. steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
@@ -304,7 +305,8 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
  *   W   dev bf16 [2 F, K]: the F rows of the gate, then those of the other factor
  *   act CHORUS_ACT_GELU (tanh form, as the block's) or CHORUS_ACT_SILU
  *   H   dev bf16 [M, F]; both projections stay in fp32 until their product is rounded
- *   pre dev bf16 [M, 2 F] or NULL: both projections, rounded, for the backward pass
+ *   pre dev 16-bit words [M, 2 F] or NULL: both projections for the backward pass, in a format of its own: 9 bits behind the point, magnitudes
+ *       from 2^-40 to 2^24; smaller ones are 0, larger ones and what is not finite come back as NaN
  *
  * chorus_gated_ffn_backward: from dH (dev bf16 [M, F], the gradient of H) and pre,
  *   dX  dev bf16 [M, K] or NULL

@@ -739,7 +739,8 @@ def chorus_attention_bias_workspace_bytes(a: BiasAttention) -> int:
 
 def chorus_attention_bias(Q, K, V, O, table, bucket, lens=None, first=None, causal=False, scale=1.0, lse=None, rest=None, ws=None):
     """O = softmax(scale Q K^T + table[bucket of the distance]) V. Q, O [B, Lq, H, dh], K, V [B, Lk, Hk, dh], rows any distance apart; lens int32 [B]:
-    keys of each sequence; first int32 [B]: position of query 0 among the keys; lse [B, H, Lq] and rest (as O) for the backward pass."""
+    keys of each sequence; first int32 [B]: position of query 0 among the keys; lse [B, H, Lq] and rest (laid out as O, the
+    other half of the result's bits) for the backward pass."""
     lib = load()
     a = _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest)
     if ws is None:
@@ -776,8 +777,15 @@ def chorus_attention_bias_backward(Q, K, V, O, rest, lse, dO, table, bucket, dQ,
 ACT_GELU, ACT_SILU = 0, 1
 
 
+def _chk_words(t, name, shape):
+    """16-bit words that one call writes for another, in a tensor of whichever type of that size."""
+    if t is not None:
+        _chk(t, t.dtype if t.dtype in (torch.bfloat16, torch.int16, torch.uint16) else torch.int16, name, shape)
+
+
 def chorus_gated_ffn(X, W, act, H, pre=None):
-    """H = act(X Wg^T) * (X Wu^T); W [2F, K] the rows of the gate, then of the other factor. pre [M, 2F]: both projections, for the backward pass."""
+    """H = act(X Wg^T) * (X Wu^T); W [2F, K] the rows of the gate, then of the other factor. pre [M, 2F], 16-bit words: both projections as the backward
+    pass reads them."""
     lib = load()
     _chk(X, torch.bfloat16, "X")
     _chk(W, torch.bfloat16, "W")
@@ -785,7 +793,7 @@ def chorus_gated_ffn(X, W, act, H, pre=None):
     if W.shape != (2 * F, K):
         raise TypeError("X/W dimensions differ")
     _chk(H, torch.bfloat16, "H", (M, F))
-    _chk(pre, torch.bfloat16, "pre", (M, 2 * F))
+    _chk_words(pre, "pre", (M, 2 * F))
     _status("chorus_gated_ffn", lib.chorus_gated_ffn(_p(X), _p(W), int(act), _p(H), _p(pre), M, F, K, _stream()))
     return H
 
@@ -802,7 +810,7 @@ def chorus_gated_ffn_backward(X, W, pre, dH, act, dX, dW, accumulate=False, ws=N
     (M, K), F = X.shape, W.shape[0] // 2
     if W.shape != (2 * F, K):
         raise TypeError("X/W dimensions differ")
-    _chk(pre, torch.bfloat16, "pre", (M, 2 * F))
+    _chk_words(pre, "pre", (M, 2 * F))
     _chk(dH, torch.bfloat16, "dH", (M, F))
     _chk(dX, torch.bfloat16, "dX", (M, K))
     full = accumulate or (dW is not None and dW.dtype == torch.float32)

@@ -141,6 +141,16 @@ __device__ __forceinline__ float lane_value(int src, float v) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)__float_as_uint(v)));
 }
 
+// The 16 bits of an fp32 value that its rounding to bf16 leaves off, as the whole number that the rounded one's bits, 16 places further up, are short of
+// the value's: both together are the value, but for a half that was rounded down, which is short of one in the last place.
+__device__ __forceinline__ uint16_t left_off(float v) {
+  const int d = (int)(__float_as_uint(v) - ((uint32_t)f32_to_bf16(v) << 16));
+  return (uint16_t)(d < 0x7fff ? d : 0x7fff);
+}
+__device__ __forceinline__ float both_halves(uint16_t rounded, uint16_t rest) {
+  return __uint_as_float(((uint32_t)rounded << 16) + (uint32_t)(int)(int16_t)rest);
+}
+
 bool bias_step_ok(int64_t row, int64_t batch, int64_t heads, int32_t dh);
 int32_t check_bias_sizes(const chorus_bias_attention* a);
 // The checks that both directions share; sets the kernels' view.

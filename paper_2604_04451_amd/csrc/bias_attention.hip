@@ -29,17 +29,18 @@ size_t slice_bytes(long tiles, int slices, int dh, int rows) {
 
 struct Outputs {
   RowsOut o;
-  uint16_t* rest;  // as o
+  uint16_t* rest;  // as o, the other half of the bits
   float* lse;      // [B, H, Lq]
 };
 
-// SPLIT: for the backward pass, whose sums of gradients by bucket cancel to a small part of their terms, a weight's rounding is made up for by a
-// second product with what it left off (16 bits of a weight altogether), and so is that of the result by a second output.
+// SPLIT: for the backward pass, whose sums of gradients by bucket cancel to a small part of their terms (relative error of the table's gradient, 8 x 512
+// tokens: 2.5e-6 with weights of 16 bits, 5.7e-7 with 24, 5.3e-7 with fp32 products; 7 % of a training step), a weight goes to the matrix pipe in
+// three parts of 8 bits, and the other half of the result's bits goes out as well.
 template <int DH, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
                                                                 long Lk, int H, int group, int nq, int slices) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the buffer descriptors below are types of the device compiler's alone
-  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2;
+  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2, PARTS = SPLIT ? 3 : 1;
   constexpr int TILE = kTileKeys * DH;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values, biases
   float* const s_bias = reinterpret_cast<float*>(smem + 4 * TILE);
@@ -199,26 +200,28 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
     __builtin_amdgcn_sched_barrier(0);
     logits(t);
     move();
-    bf16x8 pf[NC][RB], pl[NC][RB];
+    bf16x8 pf[PARTS][NC][RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
+          float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
           l_run[rb] += p;
-          pf[c][rb][e] = (bf16_t)p;
-          if (SPLIT) pl[c][rb][e] = (bf16_t)(p - (float)pf[c][rb][e]);
+#pragma unroll
+          for (int a = 0; a < PARTS; ++a) {
+            pf[a][c][rb][e] = (bf16_t)p;
+            p -= (float)pf[a][c][rb][e];
+          }
         }
       }
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        asm volatile("" : "+v"(pf[c][rb]));  // here and not where they are used
-        if (SPLIT) asm volatile("" : "+v"(pl[c][rb]));
-      }
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int a = 0; a < PARTS; ++a) asm volatile("" : "+v"(pf[a][c][rb]));  // here and not where they are used
     // what was requested a step ago: the keys behind the next tile's over this tile's, whose logits are made, the next tile's values
     // beside this one's
     if (t + 2 < t1) k_in.store(smem + buf * TILE);
@@ -243,8 +246,8 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
       for (int u = 0; u < 2; ++u) {
         if (i < VS) {
           const int db = i / NC, rb = i % NC, c = u;
-          o[db][rb] = mfma(fr[db * NC + c], pf[c][rb], o[db][rb]);
-          if (SPLIT) o[db][rb] = mfma(fr[db * NC + c], pl[c][rb], o[db][rb]);
+#pragma unroll
+          for (int a = 0; a < PARTS; ++a) o[db][rb] = mfma(fr[db * NC + c], pf[a][c][rb], o[db][rb]);
         } else {
           const int kb = (i - VS) / KC, at = (i - VS) % KC * 2 + u, rb = at / KC, kc = at % KC;
           if (kc == 0) s[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -291,16 +294,12 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
       for (int i = 0; i < DB / 2; ++i) {
         // 4 values of block 2i and 4 of 2i + 1 here, and as many with the lane 16 further: after the swap eight of the one here, of
         // the other there
-        f32x4 x = o[2 * i][rb] * inv, y = o[2 * i + 1][rb] * inv;
-        if (SPLIT && rest) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[e] -= bf16_to_f32(f32_to_bf16(x[e]));
-            y[e] -= bf16_to_f32(f32_to_bf16(y[e]));
-          }
-        }
-        const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[0], x[1]), pack_bf16x2(y[0], y[1]), false, false);
-        const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(x[2], x[3]), pack_bf16x2(y[2], y[3]), false, false);
+        const f32x4 x = o[2 * i][rb] * inv, y = o[2 * i + 1][rb] * inv;
+        const auto two = [&](float a, float b) {
+          return SPLIT && rest ? (uint32_t)left_off(a) | (uint32_t)left_off(b) << 16 : pack_bf16x2(a, b);
+        };
+        const auto lo = __builtin_amdgcn_permlane16_swap(two(x[0], x[1]), two(y[0], y[1]), false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(two(x[2], x[3]), two(y[2], y[3]), false, false);
         const u32x4 v = {from_lane(src, lo[0]), from_lane(src, hi[0]), from_lane(src, lo[1]), from_lane(src, hi[1])};
         if (live) *reinterpret_cast<u32x4*>(p + to + 32 * i) = v;
       }
@@ -340,9 +339,8 @@ __global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict_
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float v = sum[e] * inv;
-    const uint16_t r = f32_to_bf16(v);
-    out.o.p[to + e] = r;
-    if (out.rest) out.rest[to + e] = f32_to_bf16(v - bf16_to_f32(r));
+    out.o.p[to + e] = f32_to_bf16(v);
+    if (out.rest) out.rest[to + e] = left_off(v);
   }
   if (out.lse && lane == 0) out.lse[bh * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }

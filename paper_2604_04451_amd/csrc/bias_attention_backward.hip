@@ -102,9 +102,10 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dq_kernel(Rows Q, 
     for (int kc = 0; kc < KC; ++kc) {
       qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
       df[rb][kc] = *reinterpret_cast<const bf16x8*>(dp + 32 * kc);
-      const bf16x8 o = *reinterpret_cast<const bf16x8*>(O.p + at + 32 * kc), r = *reinterpret_cast<const bf16x8*>(rest + at + 32 * kc);
+      const u32x4 o = *reinterpret_cast<const u32x4*>(O.p + at + 32 * kc), r = *reinterpret_cast<const u32x4*>(rest + at + 32 * kc);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf((float)df[rb][kc][e], (float)o[e] + (float)r[e], sum);
+      for (int e = 0; e < 8; ++e)
+        sum = __builtin_fmaf((float)df[rb][kc][e], both_halves((uint16_t)(o[e / 2] >> 16 * (e % 2)), (uint16_t)(r[e / 2] >> 16 * (e % 2))), sum);
     }
     sum += swap_rows16(sum);
     sum += swap_halves(sum);

@@ -321,43 +321,25 @@ struct EpiArgs {
   float scale;
 };
 
-// bf16 (optionally GELU) epilogue of the 16x16 layout: 32 output rows at a time go through a private LDS region as
-// [32][16 WBN] bf16 (row stride 16 WBN + 8), then leave as full row segments of the quadrant (256, 128 or 64 bytes). ld: values from
-// row to row of the output.
+// Results of 16 bits on their way out: 32 output rows at a time go through a private LDS region as [32][16 WBN] (row stride 16 WBN + 8), then
+// leave as full row segments of the quadrant (256, 128 or 64 bytes). words(nb, mb): a lane's four values of a block. ld: values from row to
+// row of the output.
 template <int WBN> constexpr int e16_bf_stride() { return 16 * WBN + 8; }
 template <int WBN> constexpr int e16_bf_wave() { return 32 * e16_bf_stride<WBN>(); }  // elements per wave
-template <int EPI, int WBM, int WBN, class BLOCK>
-__device__ __forceinline__ void gemm16_epilogue_bf16(const BLOCK& block, const EpiArgs& ep, uint16_t* cw, long m_wave0,
-                                                     int n_wave0, long M, int N, long ld, int lane) {
+template <int WBM, int WBN, class WORDS>
+__device__ __forceinline__ void gemm16_rows_out(const WORDS& words, uint16_t* out, uint16_t* cw, long m_wave0, int n_wave0, long M, int N, long ld,
+                                                int lane) {
   constexpr int E16_BF_STRIDE = e16_bf_stride<WBN>();
   constexpr int LPR = 2 * WBN, RPI = 64 / LPR;  // read-back: LPR lanes x 16 bytes per row, RPI rows per instruction
   const int lj = lane & 15, lg = lane >> 4;
   const int rrow = lane / LPR, rcol = (lane % LPR) * 8;
-  float4 bias[WBN];
-#pragma unroll
-  for (int nb = 0; nb < WBN; ++nb) {
-    const int n = n_wave0 + 16 * nb + 4 * lg;
-    bias[nb] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (ep.bias && n < N) bias[nb] = *reinterpret_cast<const float4*>(ep.bias + n);
-  }
 #pragma unroll
   for (int mp = 0; mp < WBM / 2; ++mp) {  // pairs of 16-row blocks
 #pragma unroll
     for (int mh = 0; mh < 2; ++mh)
 #pragma unroll
-      for (int nb = 0; nb < WBN; ++nb) {
-        f32x4 a = block(nb, 2 * mp + mh);
-        // one block at a time out of the accumulators: of the large tile's, fetched together, 8 to 12 bytes a lane spilled
-        if (WBM == 8 && mh) asm volatile("" : "+v"(a));
-        float v0 = a[0] + bias[nb].x, v1 = a[1] + bias[nb].y, v2 = a[2] + bias[nb].z, v3 = a[3] + bias[nb].w;
-        if (EPI == CHORUS_EPI_GELU_BF16) {
-          v0 = gelu_tanh_fast(v0); v1 = gelu_tanh_fast(v1); v2 = gelu_tanh_fast(v2); v3 = gelu_tanh_fast(v3);
-        }
-        uint2 w;
-        w.x = pack_bf16x2(v0, v1);
-        w.y = pack_bf16x2(v2, v3);
-        *reinterpret_cast<uint2*>(cw + (16 * mh + lj) * E16_BF_STRIDE + 16 * nb + 4 * lg) = w;
-      }
+      for (int nb = 0; nb < WBN; ++nb)
+        *reinterpret_cast<uint2*>(cw + (16 * mh + lj) * E16_BF_STRIDE + 16 * nb + 4 * lg) = words(nb, 2 * mp + mh);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
 #pragma unroll
     for (int it = 0; it < 32 / RPI; ++it) {
@@ -367,11 +349,36 @@ __device__ __forceinline__ void gemm16_epilogue_bf16(const BLOCK& block, const E
       const u32x4 v = *reinterpret_cast<const u32x4*>(cw + row * E16_BF_STRIDE + rcol);
       // streaming store: an output tile is not read again by this kernel, and left to the default policy the written
       // lines push the operand panels that the next tiles share out of the L2 (measured: 14-19 % on the widest output)
-      if (m < M && n < N) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(ep.out) + m * ld + n));
+      if (m < M && n < N) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out + m * ld + n));
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_sched_barrier(0);
   }
+}
+
+// bf16 (optionally GELU) epilogue of the 16x16 layout, block(nb, mb) being a lane's part of a block of results
+template <int EPI, int WBM, int WBN, class BLOCK>
+__device__ __forceinline__ void gemm16_epilogue_bf16(const BLOCK& block, const EpiArgs& ep, uint16_t* cw, long m_wave0, int n_wave0, long M, int N,
+                                                     int lane) {
+  const int lg = lane >> 4;
+  float4 bias[WBN];
+#pragma unroll
+  for (int nb = 0; nb < WBN; ++nb) {
+    const int n = n_wave0 + 16 * nb + 4 * lg;
+    bias[nb] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (ep.bias && n < N) bias[nb] = *reinterpret_cast<const float4*>(ep.bias + n);
+  }
+  const auto words = [&](int nb, int mb) {
+    f32x4 a = block(nb, mb);
+    // one block at a time out of the accumulators: of the large tile's, fetched together, 8 to 12 bytes a lane spilled
+    if (WBM == 8 && (mb & 1)) asm volatile("" : "+v"(a));
+    float v0 = a[0] + bias[nb].x, v1 = a[1] + bias[nb].y, v2 = a[2] + bias[nb].z, v3 = a[3] + bias[nb].w;
+    if (EPI == CHORUS_EPI_GELU_BF16) {
+      v0 = gelu_tanh_fast(v0); v1 = gelu_tanh_fast(v1); v2 = gelu_tanh_fast(v2); v3 = gelu_tanh_fast(v3);
+    }
+    return make_uint2(pack_bf16x2(v0, v1), pack_bf16x2(v2, v3));
+  };
+  gemm16_rows_out<WBM, WBN>(words, reinterpret_cast<uint16_t*>(ep.out), cw, m_wave0, n_wave0, M, N, N, lane);
 }
 
 // fp32 gated-residual epilogue of the 16x16 layout: 16 output rows at a time through a private LDS region as
@@ -453,7 +460,7 @@ __device__ __forceinline__ void gemm16_finish(const BLOCK& block, const EpiArgs&
   uint16_t* smem = reinterpret_cast<uint16_t*>(smem_raw);
   const int lj = lane & 15, lg = lane >> 4;
   if constexpr (EPI == CHORUS_EPI_BF16 || EPI == CHORUS_EPI_GELU_BF16) {
-    gemm16_epilogue_bf16<EPI, WBM, WBN>(block, ep, smem + wave * e16_bf_wave<WBN>(), m0 + wm * WTM, n0 + wn * WTN, M, N, N, lane);
+    gemm16_epilogue_bf16<EPI, WBM, WBN>(block, ep, smem + wave * e16_bf_wave<WBN>(), m0 + wm * WTM, n0 + wn * WTN, M, N, lane);
   } else if constexpr (EPI == CHORUS_EPI_RESID) {
     gemm16_epilogue_resid<WBM, WBN>(block, ep, reinterpret_cast<float*>(smem_raw) + wave * e16_f32_wave<WBN>(), m0 + wm * WTM,
                                     n0 + wn * WTN, M, N, lane);
