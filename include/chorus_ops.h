@@ -256,7 +256,7 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *
  * chorus_bias_attention
  *   B, Lq, Lk, H, Hk, dh   sequences, queries and keys of each, heads, heads of keys and values (H % Hk == 0; head h reads h / (H / Hk)); dh in {64, 128}
- *   n_buckets, far         rows of the table; distance from which on all share the bucket at the end, 0 to 1024
+ *   n_buckets, far         rows of the table; distance from which on all share the bucket at the end, 0 to 512
  *   causal, scale          scale > 0, finite
  *   *_row, *_batch         steps in values, multiples of 8; a row step at least heads * dh and at most 2^23
  * chorus_bias_buckets: host only; the usual map: bucket host [2 far + 1], the buckets of distances -far .. far. One bucket each for the
@@ -266,10 +266,9 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
  *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
  *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass
- *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass (whose
- *               sums by bucket cancel to a small part of their terms). With it the weights count with 24 bits.
+ *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
- *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe (without rest).
+ *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe.
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
  *   dtable dev fp32 [n_buckets, H]. steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.

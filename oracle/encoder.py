@@ -122,7 +122,9 @@ def attention_bias_backward(q, k, v, table, bucket, lens, first, causal, scale, 
             dv[b, :, g] += p.T @ d
             np.add.at(dtable[:, h], of.ravel(), ds.ravel())
             a = np.abs(ds) + 2.0 ** -6 * size
-            mq[b, :, h] = a @ np.abs(k[b, :, g]) * scale
+            # in the products for dq delta has the roundings of o's weights in it, to 8 bits
+            row = (np.abs(d) * (p @ np.abs(v[b, :, g]))).sum(1, keepdims=True)
+            mq[b, :, h] = (a + p * row) @ np.abs(k[b, :, g]) * scale
             mk[b, :, g] += a.T @ np.abs(q[b, :, h]) * scale
             mv[b, :, g] += p.T @ np.abs(d)
             np.add.at(mt[:, h], of.ravel(), size.ravel())

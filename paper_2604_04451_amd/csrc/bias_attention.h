@@ -6,9 +6,9 @@
 namespace chorus {
 
 constexpr int kTileKeys = 64;      // keys (or, where keys stand still, queries) of a step, in LDS
-constexpr int kTileQueries = 128;  // queries (or keys) of a workgroup: four waves of 32
+constexpr int kTileQueries = 128;  // queries (or keys) of a workgroup
 constexpr int kPad = 96;           // a near tile's distances reach 63 + 31 behind the farthest
-constexpr int kMostFar = 1024;
+constexpr int kMostFar = 512;  // biases and a wave's sums of every distance fit the LDS beside the tiles
 constexpr int64_t kMostTokens = 1 << 28;
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -69,9 +69,9 @@ __device__ __forceinline__ void* uniform(const void* p) {
 // 64 rows of DH values on their way from global memory to LDS, through registers: a copy straight into LDS would make the compiler wait for
 // all of them ahead of every transposing read. Each thread fetches the 16 bytes that belong at its place of the tile. Rows behind the last are
 // the last one again: nothing behind it is read.
-template <int DH>
+template <int DH, int THREADS>
 struct TileStage {
-  static constexpr int kLoads = DH / 32, kPieces = DH / 8, kRows = 256 / kPieces;  // of a thread for a tile; of a row; of the workgroup's loads
+  static constexpr int kPieces = DH / 8, kRows = THREADS / kPieces, kLoads = kTileKeys / kRows;  // of a row; of the workgroup's loads; of a thread for a tile
   int row, piece, row_bytes, to;
   u32x4 v[kLoads];
   __device__ __forceinline__ TileStage(int tid, long row_step) {
@@ -91,7 +91,7 @@ struct TileStage {
   }
   __device__ __forceinline__ void store(uint16_t* tile) const {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(tile + to + i * 2048) = v[i];
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(tile + to + i * (THREADS * 8)) = v[i];
   }
 };
 #endif

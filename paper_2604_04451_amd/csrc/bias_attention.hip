@@ -33,14 +33,13 @@ struct Outputs {
   float* lse;      // [B, H, Lq]
 };
 
-// SPLIT: for the backward pass, whose sums of gradients by bucket cancel to a small part of their terms (relative error of the table's gradient, 8 x 512
-// tokens: 2.5e-6 with weights of 16 bits, 5.7e-7 with 24, 5.3e-7 with fp32 products; 7 % of a training step), a weight goes to the matrix pipe in
-// three parts of 8 bits, and the other half of the result's bits goes out as well.
+// SPLIT: for the backward pass a weight goes to the matrix pipe in two parts of 8 bits, and the other half of the result's bits goes out as well: delta =
+// dO . O then has 16 bits (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of 8 bits; SPLITCOST).
 template <int DH, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
                                                                 long Lk, int H, int group, int nq, int slices) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the buffer descriptors below are types of the device compiler's alone
-  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2, PARTS = SPLIT ? 3 : 1;
+  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2, PARTS = SPLIT ? 2 : 1;
   constexpr int TILE = kTileKeys * DH;
   extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values, biases
   float* const s_bias = reinterpret_cast<float*>(smem + 4 * TILE);
@@ -61,7 +60,7 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
   const int steps = (most + kTileKeys - 1) / kTileKeys;
   const int t0 = (int)((long)steps * slice / slices), t1 = (int)((long)steps * (slice + 1) / slices);
 
-  TileStage<DH> k_in(tid, K.row), v_in(tid, V.row);
+  TileStage<DH, 256> k_in(tid, K.row), v_in(tid, V.row);
   const uint16_t* const k_base = K.p + (long)b * K.batch + (long)(head / group) * DH;
   const uint16_t* const v_base = V.p + (long)b * V.batch + (long)(head / group) * DH;
   auto fetch_k = [&](int t) { k_in.fetch(k_base + (long)t * kTileKeys * K.row, n - 1 - t * kTileKeys); };
@@ -207,13 +206,10 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
       for (int c = 0; c < NC; ++c) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
+          const float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
           l_run[rb] += p;
-#pragma unroll
-          for (int a = 0; a < PARTS; ++a) {
-            pf[a][c][rb][e] = (bf16_t)p;
-            p -= (float)pf[a][c][rb][e];
-          }
+          pf[0][c][rb][e] = (bf16_t)p;
+          if (SPLIT) pf[PARTS - 1][c][rb][e] = (bf16_t)(p - (float)pf[0][c][rb][e]);
         }
       }
 #pragma unroll

@@ -1,7 +1,11 @@
 // Gradients of attention with a bias by distance. With P the weights, made again from the logits and the rows' logarithms of their sums,
-//   delta_i = dO_i . O_i,  dS = P (dO V^T - delta),  dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K,  dtable[c] = sum of dS where the bucket is c.
-// Two passes over the logits, neither of which adds to memory that another workgroup adds to: queries stand still in the first (dQ, the
-// sums of dS by distance, delta), keys in the second (dK and dV, over all heads that share them). A third kernel adds up the distances' sums.
+//   delta_i = sum_j P_ij (dO V^T)_ij = dO_i . O_i,  dS = P (dO V^T - delta),  dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K,
+//   dtable[c] = sum of dS where the bucket is c.
+// Two passes over the logits, neither of which adds to memory that another workgroup adds to: queries stand still in the first (dQ), keys in
+// the second (dK and dV, over all heads that share them, and the sums of dS by distance). Two small kernels add up the distances' sums.
+// The sums over a bucket cancel to a small part of their terms, and an error of delta goes into all terms of a row alike. O has the roundings of
+// the forward pass's weights in it; but a row's dS add up to 0, so that what those of the first pass add up to is what its delta was off by, and the
+// second pass has it to fp32 (table's gradient, 8 x 512 tokens: relative error KNOWN).
 #include "bias_attention.h"
 
 namespace chorus {
@@ -34,34 +38,31 @@ __device__ __forceinline__ void put_columns(const f32x4 (&x)[DB], float factor, 
 __device__ __forceinline__ float row_exponent(float lse, bool live) { return live && lse > -INFINITY ? lse * kLog2E : INFINITY; }
 
 // ---------------------------------------------------------------------------
-// Queries stand still: as the forward kernel, 32 queries a wave, keys 64 at a time. The products S^T = K Q^T and dP^T = V dO^T leave a lane with
-// a query's logits and their gradients as the operand of dQ^T += K^T dS^T.
-// Sums by distance: a wave's 64 x 32 gradients of a near tile are added up along their diagonals. Blocks of 16 x 16 on one diagonal are added
-// in registers first, five diagonals of blocks; they go to LDS with row c of 16 shifted c places to the left, so that a column
-// of the 95 places is a distance, and two places a lane are summed and added to the wave's own sums of distances. Tiles whose
-// distances all share an end bucket cost one addition a value.
+// Queries stand still: eight waves of 16 queries in registers, keys and values 64 at a time through LDS. The products S^T = K Q^T and dP^T = V dO^T leave a
+// lane with a query's logits and their gradients as the operand of dQ^T += K^T dS^T. Fragments are read some slots before the MFMAs that use them, in
+// the order written: left to itself the compiler reads them as they are needed, and a wave waits for the LDS at every one.
+// Two waves on a SIMD take turns with the vector and the matrix pipe. With 32 queries a wave half the LDS reads would do, but one wave a SIMD is all that
+// the registers hold then (heads of 128, 8191 tokens: first pass 788 us, second 1104; so FIRST and SECOND).
 // ---------------------------------------------------------------------------
-constexpr int kSkewPlaces = 95, kSkewRow = 97;
+constexpr int kWaves = 8;
 
 template <int DH>
-__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dq_kernel(Rows Q, Rows K, Rows V, Rows O, const uint16_t* __restrict__ rest, Rows dO, RowsOut dQ,
-                                                         const float* __restrict__ lse, Delta delta, float* __restrict__ part, BiasArgs bias, long Lq,
-                                                         long Lk, int H, int group, int nq) {
+__global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(Rows Q, Rows K, Rows V, Rows O, const uint16_t* __restrict__ rest, Rows dO,
+                                                                                RowsOut dQ, const float* __restrict__ lse, Delta delta, BiasArgs bias,
+                                                                                long Lq, long Lk, int H, int group, int nq) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2;
+  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, THREADS = 64 * kWaves;
   constexpr int TILE = kTileKeys * DH;
-  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values, biases, sums of each wave, skewed rows of each
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] keys, [2][TILE] values, biases
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
   const int width = bias.width(), far = bias.far;
   float* const s_bias = reinterpret_cast<float*>(smem + 4 * TILE);
-  float* const s_sums = s_bias + width + wave * width;
-  float* const s_skew = s_bias + 5 * width + wave * 16 * kSkewRow;
 
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int bh = unit / nq, qb = unit - bh * nq, b = bh / H, head = bh - b * H;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
-  const int q0 = qb * kTileQueries + wave * 32;
+  const int q0 = qb * kTileQueries + wave * 16;
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
   int most = n;
   if (bias.causal) {
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dq_kernel(Rows Q, 
   }
   const int steps = (most + kTileKeys - 1) / kTileKeys;
 
-  TileStage<DH> k_in(tid, K.row), v_in(tid, V.row);
+  TileStage<DH, THREADS> k_in(tid, K.row), v_in(tid, V.row);
   const uint16_t* const k_base = K.p + (long)b * K.batch + (long)(head / group) * DH;
   const uint16_t* const v_base = V.p + (long)b * V.batch + (long)(head / group) * DH;
   auto fetch = [&](int t) {
@@ -82,221 +83,176 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dq_kernel(Rows Q, 
     v_in.store(smem + (2 + buf) * TILE);
   };
   if (steps > 0) fetch(0);
-  for (int i = tid; i < width; i += 256) s_bias[i] = bias.bias(i, head, H);
-  for (int i = lane; i < width; i += 64) s_sums[i] = 0.f;
-  for (int i = lane; i < 16 * kSkewRow; i += 64) s_skew[i] = 0.f;
+  for (int i = tid; i < width; i += THREADS) s_bias[i] = bias.bias(i, head, H);
 
   const RowFragments<DH> rows(lane);
   const ColumnFragments<DH> columns(lane);
-  bf16x8 qf[RB][KC], df[RB][KC];
-  float ex[RB], dl[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const bool live = q0 + 16 * rb + lq < Lq;
-    const long q = live ? q0 + 16 * rb + lq : Lq - 1;
+  bf16x8 qf[KC], df[KC];
+  const bool live = q0 + lq < Lq;
+  const long q = live ? q0 + lq : Lq - 1;
+  float dl = 0.f, over = 0.f;  // delta; what the row's gradients add up to, this lane's share
+  {
     const uint16_t* qp = Q.p + (long)b * Q.batch + q * Q.row + (long)head * DH + 8 * g;
     const uint16_t* dp = dO.p + (long)b * dO.batch + q * dO.row + (long)head * DH + 8 * g;
     const long at = (long)b * O.batch + q * O.row + (long)head * DH + 8 * g;
-    float sum = 0.f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
-      df[rb][kc] = *reinterpret_cast<const bf16x8*>(dp + 32 * kc);
+      qf[kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
+      df[kc] = *reinterpret_cast<const bf16x8*>(dp + 32 * kc);
       const u32x4 o = *reinterpret_cast<const u32x4*>(O.p + at + 32 * kc), r = *reinterpret_cast<const u32x4*>(rest + at + 32 * kc);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        sum = __builtin_fmaf((float)df[rb][kc][e], both_halves((uint16_t)(o[e / 2] >> 16 * (e % 2)), (uint16_t)(r[e / 2] >> 16 * (e % 2))), sum);
+        dl = __builtin_fmaf((float)df[kc][e], both_halves((uint16_t)(o[e / 2] >> 16 * (e % 2)), (uint16_t)(r[e / 2] >> 16 * (e % 2))), dl);
     }
-    sum += swap_rows16(sum);
-    sum += swap_halves(sum);
-    dl[rb] = sum;
-    ex[rb] = row_exponent(lse[(long)bh * Lq + q], live);
-    if (g == 0 && live) delta.p[(long)bh * Lq + q] = sum;
+    dl += swap_rows16(dl);
+    dl += swap_halves(dl);
   }
-  f32x4 dq[RB][DB];
+  const float ex = row_exponent(lse[(long)bh * Lq + q], live);  // exponent of the row's sum
+  f32x4 dq[DB];
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int db = 0; db < DB; ++db) dq[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int db = 0; db < DB; ++db) dq[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (steps > 0) store(0);
   if (steps > 1) fetch(1);
   lds_barrier();
   const float below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
   const float above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
   const float scale = bias.scale * kLog2E;
-  float sum_below = 0.f, sum_above = 0.f;
 
   for (int t = 0, buf = 0; t < steps; ++t, buf ^= 1) {
     if (t + 1 < steps) store(buf ^ 1);
     if (t + 2 < steps) fetch(t + 2);
     const uint16_t* const k_tile = smem + buf * TILE;
     const uint16_t* const v_tile = smem + (2 + buf) * TILE;
-    f32x4 s[KB][RB], dp[KB][RB];
+    f32x4 s[KB], dp[KB];
+    {
+      constexpr int SLOTS = KB * KC, kAhead = 4;
+      bf16x8 kf[SLOTS], vf[SLOTS];
+      auto read = [&](int f) {
+        kf[f] = rows.read(k_tile, f / KC, f % KC);
+        vf[f] = rows.read(v_tile, f / KC, f % KC);
+      };
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+      for (int f = 0; f < kAhead; ++f) read(f);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        s[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        dp[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
-        const bf16x8 kf = rows.read(k_tile, kb, kc), vf = rows.read(v_tile, kb, kc);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          s[kb][rb] = mfma(kf, qf[rb][kc], s[kb][rb]);
-          dp[kb][rb] = mfma(vf, df[rb][kc], dp[kb][rb]);
-        }
+      for (int f = 0; f < SLOTS; ++f) {
+        const int kb = f / KC, kc = f % KC;
+        if (f + kAhead < SLOTS) read(f + kAhead);
+        if (kc == 0) s[kb] = dp[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s[kb] = mfma(kf[f], qf[kc], s[kb]);
+        dp[kb] = mfma(vf[f], df[kc], dp[kb]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    const int nearest = t * kTileKeys - (origin + q0);
-    const bool near = nearest + 63 > -far && nearest - 31 < far;
-    if (near) {
+    constexpr int SLOTS2 = DB * NC, kAhead2 = 4;
+    bf16x8 kt[SLOTS2];
+    auto read2 = [&](int f) { kt[f] = columns.read(k_tile, f % NC, f / NC); };
+#pragma unroll
+    for (int f = 0; f < kAhead2; ++f) read2(f);
+    __builtin_amdgcn_sched_barrier(0);
+    const int nearest = t * kTileKeys - (origin + q0);  // distance of the tile's first key from the wave's first query
+    if (nearest + 63 > -far && nearest - 15 < far) {
       const float* at = s_bias + (nearest + far + kPad + 4 * g - lq);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, at[16 * (kb - rb) + i] - ex[rb]);
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i] - ex);
     } else {
-      const float c = nearest > 0 ? above : below;
+      const float c = (nearest > 0 ? above : below) - ex;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, c - ex[rb]);
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, c);
     }
-    int end = n;
+    int end = n;  // first key that the wave's first query does not see
     if (bias.causal && origin + q0 + 1 < end) end = origin + q0 + 1;
     if ((t + 1) * kTileKeys > end) {
+      int left = n;
+      if (bias.causal && origin + q0 + lq + 1 < n) left = origin + q0 + lq + 1;
+      left -= t * kTileKeys + 4 * g;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        int left = n;
-        if (bias.causal && origin + q0 + 16 * rb + lq + 1 < n) left = origin + q0 + 16 * rb + lq + 1;
-        left -= t * kTileKeys + 4 * g;
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (16 * kb + i >= left) s[kb][rb][i] = -INFINITY;
-      }
+        for (int i = 0; i < 4; ++i)
+          if (16 * kb + i >= left) s[kb][i] = -INFINITY;
     }
+    bf16x8 ds[NC];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_amdgcn_exp2f(s[kb][rb][i]) * (dp[kb][rb][i] - dl[rb]);
-    bf16x8 ds[NC][RB];
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ds[c][rb][e] = (bf16_t)s[2 * c + (e >> 2)][rb][e & 3];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 kf = columns.read(k_tile, c, db);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) dq[rb][db] = mfma(kf, ds[c][rb], dq[rb][db]);
+      for (int i = 0; i < 4; ++i) {
+        const float v = __builtin_amdgcn_exp2f(s[kb][i]) * (dp[kb][i] - dl);
+        over += v;
+        ds[kb / 2][4 * (kb % 2) + i] = (bf16_t)v;
       }
-    if (near) {
-      static_assert(KB == 4 && RB == 2, "five diagonals of blocks");
-      float* const row = s_skew + lq * kSkewRow + 15 - lq + 4 * g;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < 5; ++d) {  // kb - rb = d - 1
-        f32x4 v;
-        if (d == 0) v = s[0][1];
-        else if (d == 4) v = s[3][0];
-        else v = s[d % 4][1] + s[(d + 3) % 4][0];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) row[16 * d + i] = v[i];
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-      float* const sums = s_sums + nearest - 31 + far + kPad;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int p = lane + 64 * half;
-        if (p < kSkewPlaces) {
-          float a = 0.f;
-#pragma unroll
-          for (int c = 0; c < 16; ++c) a += s_skew[c * kSkewRow + p];
-          sums[p] += a;
-        }
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    } else {
-      float a = 0.f;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) a += s[kb][rb][i];
-      if (nearest > 0) sum_above += a;
-      else sum_below += a;
+    for (int f = 0; f < SLOTS2; ++f) {
+      if (f + kAhead2 < SLOTS2) read2(f + kAhead2);
+      dq[f / NC] = mfma(kt[f], ds[f % NC], dq[f / NC]);
+      __builtin_amdgcn_sched_barrier(0);
     }
     lds_barrier();
   }
-  sum_below = wave_sum(sum_below);
-  sum_above = wave_sum(sum_above);
-  if (lane == 0) {
-    s_sums[0] += sum_below;
-    s_sums[width - 1] += sum_above;
-  }
-  lds_barrier();
-  for (int i = tid; i < width; i += 256) {
-    float a = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) a += s_bias[(1 + w) * width + i];
-    part[(long)unit * width + i] = a;
-  }
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const long q = q0 + 16 * rb + (lq & 12) + g;
-    put_columns<DB>(dq[rb], bias.scale, dQ.p + (long)b * dQ.batch + q * dQ.row + (long)head * DH + 8 * (lq & 3), q < Lq, lane);
-  }
+  over += swap_rows16(over);
+  over += swap_halves(over);
+  if (g == 0 && live) delta.p[(long)bh * Lq + q] = dl + over;
+  const long row = q0 + (lq & 12) + g;
+  put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3), row < Lq, lane);
 #endif
 }
 
 // ---------------------------------------------------------------------------
-// Keys stand still: 32 keys and values a wave in registers, queries and their gradients 64 at a time through LDS, over all heads that share
-// the keys. S = Q K^T and dP = dO V^T leave a lane with one key's logits as the operand of dV^T += dO^T P and dK^T += Q^T dS.
+// Keys stand still, 128 to a workgroup in registers, queries and their gradients 64 at a time through LDS, over all heads that share the keys.
+// S = Q K^T and dP = dO V^T leave a lane with a key's logits as the operand of dV^T += dO^T P and dK^T += Q^T dS. Heads of 128 leave room for 16 keys a
+// wave, eight waves; heads of 64 for 32, four waves.
+// Sums by distance: a wave's gradients of a near tile are added up along their diagonals. Blocks of 16 x 16 on one diagonal are added in registers;
+// then they go to LDS, a row for each of 16 keys, row c shifted c places, so that a column is a distance, which lanes sum and add to the wave's own sum of
+// it. Written ahead of the products with dS and summed behind them, so that nobody waits for what was written. A tile whose distances all
+// share an end bucket costs one addition a value.
 // ---------------------------------------------------------------------------
 template <int DH>
-__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dkv_kernel(Rows Q, Rows K, Rows V, Rows dO, RowsOut dK, RowsOut dV,
-                                                                         const float* __restrict__ lse, Delta delta, BiasArgs bias, long Lq, long Lk,
-                                                                         int H, int group, int nk) {
+struct KeyShape {
+  static constexpr int kBlocks = DH == 64 ? 2 : 1, kWaves = 8 / kBlocks, kThreads = 64 * kWaves;  // blocks of 16 keys of a wave
+  static constexpr int kDiagonals = 2 + kBlocks - 1, kPlaces = 16 * kDiagonals + 15, kRow = kPlaces + 2;  // of 32 queries
+  static_assert(kPlaces <= 64, "a lane a place");
+  static int lds(int width) { return 4 * kTileKeys * DH * 2 + (4 * kTileKeys + (1 + kWaves) * width + kWaves * 16 * kRow) * 4; }
+};
+
+template <int DH>
+__global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Rows Q, Rows K, Rows V, Rows dO, RowsOut dK, RowsOut dV,
+                                                                             const float* __restrict__ lse, Delta delta, float* __restrict__ part,
+                                                                             BiasArgs bias, long Lq, long Lk, int H, int group, int nk) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int QB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, NB = 2;
-  constexpr int TILE = kTileKeys * DH;
-  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] queries, [2][TILE] their gradients, [2][2][64] exponents and deltas, biases
+  typedef KeyShape<DH> Shape;
+  constexpr int QB = 2, KC = DH / 32, DB = DH / 16, NB = Shape::kBlocks, THREADS = Shape::kThreads;
+  constexpr int TILE = kTileKeys * DH, ROW = Shape::kRow;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [2][TILE] queries, [2][TILE] their gradients, [2][2][64] exponents and deltas, biases,
+                                                                   // sums of each wave, skewed rows of each
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
+  const int width = bias.width(), far = bias.far, Hk = H / group;
   float* const s_rows = reinterpret_cast<float*>(smem + 4 * TILE);
   float* const s_bias = s_rows + 4 * kTileKeys;
-  const int width = bias.width(), far = bias.far, Hk = H / group;
+  float* const s_sums = s_bias + width + wave * width;
+  float* const s_skew = s_bias + (1 + Shape::kWaves) * width + wave * 16 * ROW;
 
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int bh = unit / nk, kt = unit - bh * nk, b = bh / Hk, kv_head = bh - b * Hk;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
-  const int k0 = kt * kTileQueries + wave * 32;  // the wave's first key
+  const int k0 = kt * kTileQueries + wave * 16 * NB;  // the wave's first key
   const int tiles = (int)((Lq + kTileKeys - 1) / kTileKeys);
   int first_tile = 0;
   if (bias.causal) {
     const int q = kt * kTileQueries - origin;  // the first query that sees the workgroup's first key
     first_tile = q <= 0 ? 0 : q / kTileKeys < tiles ? q / kTileKeys : tiles;
   }
-  const int each = kt * kTileQueries < n ? tiles - first_tile : 0, steps = each * group;
+  const int each = kt * kTileQueries < n ? tiles - first_tile : 0;
+  const bool ragged = k0 + 16 * NB > n;  // a column behind the last key holds that key again: no gradients
 
-  TileStage<DH> q_in(tid, Q.row), d_in(tid, dO.row);
+  TileStage<DH, THREADS> q_in(tid, Q.row), d_in(tid, dO.row);
   float row_in = 0.f;
-  auto fetch = [&](int i) {
-    const int head = kv_head * group + i / each, t = first_tile + i % each;
+  auto fetch = [&](int head, int t) {
     q_in.fetch(Q.p + (long)b * Q.batch + (long)t * kTileKeys * Q.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
     d_in.fetch(dO.p + (long)b * dO.batch + (long)t * kTileKeys * dO.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
     if (tid < 2 * kTileKeys) {
@@ -311,7 +267,6 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dkv_kernel(Rows Q,
     d_in.store(smem + (2 + buf) * TILE);
     if (tid < 2 * kTileKeys) s_rows[buf * 2 * kTileKeys + tid] = row_in;
   };
-  if (steps > 0) fetch(0);
 
   const RowFragments<DH> rows(lane);
   const ColumnFragments<DH> columns(lane);
@@ -335,102 +290,178 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dkv_kernel(Rows Q,
       dv[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
+  for (int i = lane; i < 16 * ROW; i += 64) s_skew[i] = 0.f;
   const float scale = bias.scale * kLog2E;
-  float below = 0.f, above = 0.f;
-  if (steps > 0) store(0);
-  if (steps > 1) fetch(1);
 
-  for (int i = 0, buf = 0; i < steps; ++i, buf ^= 1) {
-    const int t = first_tile + i % each;
-    if (i % each == 0) {  // another head, other biases
-      const int head = kv_head * group + i / each;
-      if (i > 0) lds_barrier();
-      for (int w = tid; w < width; w += 256) s_bias[w] = bias.bias(w, head, H);
+  for (int in_group = 0; in_group < group; ++in_group) {
+    const int head = kv_head * group + in_group;
+    if (each > 0) fetch(head, first_tile);
+    for (int i = tid; i < width; i += THREADS) s_bias[i] = bias.bias(i, head, H);
+    for (int i = lane; i < width; i += 64) s_sums[i] = 0.f;
+    if (each > 0) store(0);
+    if (each > 1) fetch(head, first_tile + 1);
+    lds_barrier();
+    const float below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
+    const float above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
+    float sum_below = 0.f, sum_above = 0.f;
+    for (int i = 0, buf = 0; i < each; ++i, buf ^= 1) {
+      const int t = first_tile + i;
+      if (i + 1 < each) store(buf ^ 1);
+      if (i + 2 < each) fetch(head, t + 2);
+      // half of the tile's queries at a time: logits and their gradients of all of them would not leave the registers that two waves a SIMD have
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        const uint16_t* const q_tile = smem + buf * TILE + half * 32 * DH;
+        const uint16_t* const d_tile = smem + (2 + buf) * TILE + half * 32 * DH;
+        const float* const ex = s_rows + buf * 2 * kTileKeys + half * 32 + 4 * g;
+        f32x4 s[QB][NB], dp[QB][NB];
+        {
+          constexpr int SLOTS = QB * KC, kAhead = NB == 2 ? 3 : 4;
+          bf16x8 qf[SLOTS], df[SLOTS];
+          auto read = [&](int f) {
+            qf[f] = rows.read(q_tile, f / KC, f % KC);
+            df[f] = rows.read(d_tile, f / KC, f % KC);
+          };
+#pragma unroll
+          for (int f = 0; f < kAhead; ++f) read(f);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int f = 0; f < SLOTS; ++f) {
+            const int qb = f / KC, kc = f % KC;
+            if (f + kAhead < SLOTS) read(f + kAhead);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              if (kc == 0) s[qb][nb] = dp[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+              s[qb][nb] = mfma(qf[f], kf[nb][kc], s[qb][nb]);
+              dp[qb][nb] = mfma(df[f], vf[nb][kc], dp[qb][nb]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        constexpr int kAhead2 = 3;
+        bf16x8 qc[DB], dc[DB];
+        auto read2 = [&](int f) {
+          dc[f] = columns.read(d_tile, 0, f);
+          qc[f] = columns.read(q_tile, 0, f);
+        };
+#pragma unroll
+        for (int f = 0; f < kAhead2; ++f) read2(f);
+        __builtin_amdgcn_sched_barrier(0);
+        const int nearest = k0 - (origin + t * kTileKeys + 32 * half);  // distance of the wave's first key from the half's first query
+        const bool near = nearest + 16 * NB - 1 > -far && nearest - 31 < far;
+        if (near) {
+          const float* at = s_bias + (nearest + far + kPad + lq - 4 * g);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, at[16 * (nb - qb) - e]);
+        } else {
+          const float c = nearest > 0 ? above : below;
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, c);
+        }
+        if (bias.causal && nearest + 16 * NB - 1 > 0) {
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (nearest + 16 * (nb - qb) + lq - 4 * g - e > 0) s[qb][nb][e] = -INFINITY;
+        }
+        bf16x8 pf[NB], ds[NB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(ex + 16 * qb), dl = *reinterpret_cast<const f32x4*>(ex + kTileKeys + 16 * qb);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p = __builtin_amdgcn_exp2f(s[qb][nb][e] - x[e]);
+              s[qb][nb][e] = p * (dp[qb][nb][e] - dl[e]);
+              pf[nb][4 * qb + e] = (bf16_t)p;
+              ds[nb][4 * qb + e] = (bf16_t)s[qb][nb][e];
+            }
+        }
+        if (ragged) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            if (k0 + 16 * nb + lq >= n) {
+#pragma unroll
+              for (int qb = 0; qb < QB; ++qb) s[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        if (near) {
+          float* const row = s_skew + lq * (ROW + 1) + 15 - 4 * g;
+#pragma unroll
+          for (int d = 0; d < Shape::kDiagonals; ++d) {  // nb - qb = d - (QB - 1)
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              const int qb = nb - d + QB - 1;
+              if (qb >= 0 && qb < QB) v += s[qb][nb];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) row[16 * d - e] = v[e];
+          }
+        } else {
+          float a = 0.f;
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) a += (s[qb][nb][0] + s[qb][nb][1]) + (s[qb][nb][2] + s[qb][nb][3]);
+          if (nearest > 0) sum_above += a;
+          else sum_below += a;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < DB; ++f) {
+          if (f + kAhead2 < DB) read2(f + kAhead2);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            dv[nb][f] = mfma(dc[f], pf[nb], dv[nb][f]);
+            dk[nb][f] = mfma(qc[f], ds[nb], dk[nb][f]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (near) {
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+          if (lane < Shape::kPlaces) {
+            float a = 0.f;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) a += s_skew[c * ROW + lane];
+            s_sums[nearest - 31 + far + kPad + lane] += a;
+          }
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        }
+      }
       lds_barrier();
-      below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
-      above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
     }
-    if (i + 1 < steps) store(buf ^ 1);
-    if (i + 2 < steps) fetch(i + 2);
-    const uint16_t* const q_tile = smem + buf * TILE;
-    const uint16_t* const d_tile = smem + (2 + buf) * TILE;
-    const float* const ex = s_rows + buf * 2 * kTileKeys;
-    f32x4 s[QB][NB], dp[QB][NB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        s[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        dp[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
-        const bf16x8 qf = rows.read(q_tile, qb, kc), df = rows.read(d_tile, qb, kc);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          s[qb][nb] = mfma(qf, kf[nb][kc], s[qb][nb]);
-          dp[qb][nb] = mfma(df, vf[nb][kc], dp[qb][nb]);
-        }
-      }
+    sum_below = wave_sum(sum_below);
+    sum_above = wave_sum(sum_above);
+    if (lane == 0) {
+      s_sums[0] += sum_below;
+      s_sums[width - 1] += sum_above;
     }
-    const int nearest = k0 - (origin + t * kTileKeys);  // distance of the wave's first key from the tile's first query
-    if (nearest + 31 > -far && nearest - 63 < far) {
-      const float* at = s_bias + (nearest + far + kPad + lq - 4 * g);
+    lds_barrier();
+    for (int i = tid; i < width; i += THREADS) {
+      float a = 0.f;
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, at[16 * (nb - qb) - e]);
-    } else {
-      const float c = nearest > 0 ? above : below;
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, c);
+      for (int w = 0; w < Shape::kWaves; ++w) a += s_bias[(1 + w) * width + i];
+      part[(((long)b * H + head) * nk + kt) * width + i] = a;
     }
-    if (bias.causal && nearest + 31 > 0) {
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (nearest + 16 * (nb - qb) + lq - 4 * g - e > 0) s[qb][nb][e] = -INFINITY;
-    }
-    bf16x8 pf[NC][NB], ds[NC][NB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(ex + 16 * qb + 4 * g), dl = *reinterpret_cast<const f32x4*>(ex + kTileKeys + 16 * qb + 4 * g);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(s[qb][nb][e] - x[e]);
-          pf[qb / 2][nb][4 * (qb % 2) + e] = (bf16_t)p;
-          ds[qb / 2][nb][4 * (qb % 2) + e] = (bf16_t)(p * (dp[qb][nb][e] - dl[e]));
-        }
-    }
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const bf16x8 df = columns.read(d_tile, c, db), qf = columns.read(q_tile, c, db);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          dv[nb][db] = mfma(df, pf[c][nb], dv[nb][db]);
-          dk[nb][db] = mfma(qf, ds[c][nb], dk[nb][db]);
-        }
-      }
     lds_barrier();
   }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const long k = k0 + 16 * nb + (lq & 12) + g;
     const long at = (long)kv_head * DH + 8 * (lq & 3);
-    // Keys behind the sequence: their columns hold those of its last key
     const bool counts = k0 + 16 * nb + lq < n;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -445,39 +476,48 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void bias_dkv_kernel(Rows Q,
 #endif
 }
 
-// Adds up a head's sums by distance, a workgroup a head: over sequences and tiles of queries in order, then over the distances of a bucket.
-__global__ __launch_bounds__(256) void bias_dtable_kernel(const float* __restrict__ part, float* __restrict__ dtable, BiasArgs bias, int B, int H, int nq) {
-  __shared__ double s_sum[2 * (kMostFar + kPad) + 1];
-  const int head = blockIdx.x, width = bias.width();
-  for (int i = threadIdx.x; i < width; i += 256) {
-    double a = 0.0;
-    for (int b = 0; b < B; ++b) {
-      const float* p = part + ((long)b * H + head) * nq * width + i;
-      for (int q = 0; q < nq; ++q) a += (double)p[(long)q * width];
+// Adds up the sums by distance. First, 64 distances of a head a workgroup, whose four waves share out sequences and tiles of keys; then a wave a
+// bucket and head over the distances of the bucket. Every order depends on the sizes alone.
+__global__ __launch_bounds__(256) void bias_distances_kernel(const float* __restrict__ part, double* __restrict__ sums, int width, int B, int H, int nk) {
+  __shared__ double s_sum[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y, i = blockIdx.x * 64 + lane;
+  const long n = (long)B * nk;
+  double a = 0.0;
+  if (i < width)
+#pragma unroll 8
+    for (long k = wave; k < n; k += 4) {
+      const long b = k / nk;
+      a += (double)part[((b * H + head) * nk + (k - b * nk)) * width + i];
     }
-    s_sum[i] = a;
-  }
+  s_sum[wave][lane] = a;
   __syncthreads();
-  for (int c = threadIdx.x; c < bias.n_buckets; c += 256) {
-    double a = 0.0;
-    for (int i = 0; i < width; ++i) {
-      int at = i - kPad;
-      at = at < 0 ? 0 : at > 2 * bias.far ? 2 * bias.far : at;
-      if (bias.bucket[at] == c) a += s_sum[i];
-    }
-    dtable[(long)c * H + head] = (float)a;
+  if (wave == 0 && i < width) sums[(long)head * width + i] = (s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane]);
+}
+__global__ __launch_bounds__(256) void bias_dtable_kernel(const double* __restrict__ sums, float* __restrict__ dtable, BiasArgs bias, int H) {
+  const int lane = threadIdx.x & 63, c = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, width = bias.width();
+  if (c >= bias.n_buckets) return;
+  double a = 0.0;
+  for (int i = lane; i < width; i += 64) {
+    int at = i - kPad;
+    at = at < 0 ? 0 : at > 2 * bias.far ? 2 * bias.far : at;
+    if (bias.bucket[at] == c) a += sums[(long)head * width + i];
   }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) a += __shfl_xor(a, d);
+  if (lane == 0) dtable[(long)c * H + head] = (float)a;
 }
 
 struct BackwardLayout {
-  size_t delta, part, all;
+  size_t delta, part, sums, all;
   int nq, nk;
   explicit BackwardLayout(const chorus_bias_attention& a) {
     nq = (int)((a.Lq + kTileQueries - 1) / kTileQueries);
     nk = (int)((a.Lk + kTileQueries - 1) / kTileQueries);
     delta = 0;
     part = align_up((size_t)a.B * a.H * (size_t)a.Lq * sizeof(float), 256);
-    all = part + (size_t)a.B * a.H * nq * (size_t)(2 * (a.far + kPad) + 1) * sizeof(float);
+    const size_t width = (size_t)(2 * (a.far + kPad) + 1);
+    sums = part + align_up((size_t)a.B * a.H * nk * width * sizeof(float), 256);
+    all = sums + (size_t)a.H * width * sizeof(double);
   }
 };
 
@@ -516,24 +556,28 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
   const Delta delta{reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.delta)};
   float* const part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.part);
   const int tiles = 4 * kTileKeys * a->dh * 2, most_width = 2 * (kMostFar + kPad) + 1;
-  const int lds_q = tiles + (5 * bias.width() + 4 * 16 * kSkewRow) * 4, lds_k = tiles + (4 * kTileKeys + bias.width()) * 4;
+  const int lds_q = tiles + bias.width() * 4;
   hipStream_t s = (hipStream_t)stream;
 #define BACKWARD(DH)                                                                                                                          \
   do {                                                                                                                                        \
     static DynLdsOnce once_q, once_k;                                                                                                         \
-    CHK_STATUS(once_q.ensure((const void*)bias_dq_kernel<DH>, tiles + (5 * most_width + 4 * 16 * kSkewRow) * 4));                             \
-    CHK_STATUS(once_k.ensure((const void*)bias_dkv_kernel<DH>, tiles + (4 * kTileKeys + most_width) * 4));                                    \
-    hipLaunchKernelGGL((bias_dq_kernel<DH>), dim3((unsigned)((long)a->B * a->H * at.nq)), dim3(256), lds_q, s, q, k, v, o, rest, d, gq, lse,  \
-                       delta, part, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nq);                                               \
+    CHK_STATUS(once_q.ensure((const void*)bias_dq_kernel<DH>, tiles + most_width * 4));                             \
+    CHK_STATUS(once_k.ensure((const void*)bias_dkv_kernel<DH>, KeyShape<DH>::lds(most_width)));                                    \
+    hipLaunchKernelGGL((bias_dq_kernel<DH>), dim3((unsigned)((long)a->B * a->H * at.nq)), dim3(64 * kWaves), lds_q, s, q, k, v, o, rest, d, gq, lse,  \
+                       delta, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nq);                                               \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
-    hipLaunchKernelGGL((bias_dkv_kernel<DH>), dim3((unsigned)((long)a->B * a->Hk * at.nk)), dim3(256), lds_k, s, q, k, v, d, gk, gv, lse,     \
-                       delta, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nk);                                                     \
+    hipLaunchKernelGGL((bias_dkv_kernel<DH>), dim3((unsigned)((long)a->B * a->Hk * at.nk)), dim3(KeyShape<DH>::kThreads), KeyShape<DH>::lds(bias.width()), s, q, k, v, d, gk, gv, lse,     \
+                       delta, part, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nk);                                                     \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
   } while (0)
   if (a->dh == 128) BACKWARD(128);
   else BACKWARD(64);
 #undef BACKWARD
-  hipLaunchKernelGGL(bias_dtable_kernel, dim3((unsigned)a->H), dim3(256), 0, s, (const float*)part, dtable, bias, a->B, a->H, at.nq);
+  double* const sums = reinterpret_cast<double*>(static_cast<uint8_t*>(ws) + at.sums);
+  hipLaunchKernelGGL(bias_distances_kernel, dim3((unsigned)((bias.width() + 63) / 64), (unsigned)a->H), dim3(256), 0, s, (const float*)part, sums,
+                     bias.width(), a->B, a->H, at.nk);
+  CHORUS_LAUNCH_CHECK();
+  hipLaunchKernelGGL(bias_dtable_kernel, dim3((unsigned)((a->n_buckets + 3) / 4), (unsigned)a->H), dim3(256), 0, s, (const double*)sums, dtable, bias, a->H);
   CHORUS_LAUNCH_CHECK();
   return CHORUS_OK;
 }

@@ -2,8 +2,8 @@
   weights are rounded to bf16 behind the matrix pipe's sums and the result once more: u A + u |O|, A the attention with |V| for V;
   a logit of up to 32 (in powers of two) from at most 128 products, its bias and the reference is off by at most 2^-16, of which the
   sum of the weights has as much: 2^-15 A together, 2^-10 A taken; lse: 2^-16 (1 + |lse|) for logits of that size
-  with `rest` weights and result keep 24 bits: the logits' 2^-15 A and as much for sums, 2^-13 A taken
-  gradients: a weight is off by 2^-15 of itself, the gradient of a logit, ds = p (dp - delta), by 2^-14 of size = p (|do| |v| + |do o|) and is
+  with `rest` the result is not rounded
+  gradients (delta is off by u |do| A in dq, where it comes from o, and by 2^-14 of its terms elsewhere): a weight is off by 2^-15 of itself, the gradient of a logit, ds = p (dp - delta), by 2^-14 of size = p (|do| |v| + |do o|) and is
   rounded to bf16 for the products: u |ds| + u 2^-6 size, whose sums against |k| and |q| the oracle returns (mq, mk), with those of p |do|
   (mv) and of size (mt): u of the first three, one more u of the result, 1.1 for sums in fp32; 2^-14 mt for the table, whose terms are
   not rounded to bf16."""
@@ -95,7 +95,7 @@ def check_forward(c, train=True):
         assert np.array_equal(np.isneginf(got), ~some)
         assert (np.abs(got[some] - want_lse[some]) <= 2.0 ** -16 * (1 + np.abs(want_lse[some]))).all()
         bits = (O.contiguous().view(torch.int16).int() << 16) + rest.contiguous().view(torch.int16).int()  # both halves of the fp32 result
-        assert (np.abs(host(bits.view(torch.float32)).astype(np.float64) - o) <= 2.0 ** -13 * A).all()
+        assert (np.abs(host(bits.view(torch.float32)).astype(np.float64) - o) <= U * A + 2.0 ** -10 * A).all()
         assert torch.equal(bits.view(torch.float32).to(BF), O.contiguous())
     return c
 
@@ -108,7 +108,7 @@ FORWARD = [
     dict(B_=4, H=2, Hk=2, dh=64, Lq=1, Lk=1000, causal=True, lens=[1000, 999, 64, 0], first=[999, 998, 63, -1], both=False),
     dict(B_=1, H=3, Hk=3, dh=128, Lq=16, Lk=2100), dict(B_=2, H=2, Hk=2, dh=128, Lq=17, Lk=1500, lens=[1500, 300], first=[700, 100]),
     dict(B_=1, H=2, Hk=2, dh=64, Lq=260, Lk=1300, first=[520], far=512, buckets=64), dict(B_=1, H=2, Hk=2, dh=64, Lq=90, Lk=90, far=3, buckets=4),
-    dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[-2000000000]), dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[2000000000], far=1024),
+    dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[-2000000000]), dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[2000000000], far=512),
     dict(B_=2, H=8, Hk=2, dh=64, Lq=1, Lk=777, lens=[777, 401], first=[776, 400], causal=True),
 ]
 
@@ -161,7 +161,7 @@ def test_buckets_outside_the_table_have_no_bias():
 
 
 def test_buckets_of_the_host_call():
-    for n, far, both in ((32, 128, True), (32, 128, False), (8, 8, False), (64, 512, True), (16, 1024, True), (12, 100, True), (2, 7, False), (4, 3, True)):
+    for n, far, both in ((32, 128, True), (32, 128, False), (8, 8, False), (64, 512, True), (16, 500, True), (12, 100, True), (2, 7, False), (4, 3, True)):
         assert B.chorus_bias_buckets(n, far, both).tolist() == OE.bias_buckets(n, far, both).tolist(), (n, far, both)
 
 
