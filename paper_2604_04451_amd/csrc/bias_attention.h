@@ -85,8 +85,9 @@ struct TileStage {
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(uniform(p), 0, -1, 0x00027000);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = row + i * kRows;
-      v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (r < rest ? r : rest) * row_bytes + piece, 0, 0));
+      const int r = row + i * kRows;  // row is below kRows, a power of two: their bits do not meet
+      const int from = (r < rest ? r : rest) * row_bytes + (piece ^ tile_swizzle<DH>(i * kRows) * 16);
+      v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, from, 0, 0));
     }
   }
   __device__ __forceinline__ void store(uint16_t* tile) const {

@@ -307,51 +307,275 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
 #endif
 }
 
-// Puts the slices of a row together, a wave a row: the largest reference, then the slices' results and sums by their distance from it, in
-// an order that depends on nothing but their number.
+// ---------------------------------------------------------------------------
+// Few queries: what they take is the time to read the keys and values. Up to 16 rows, the queries of as many of the heads that share keys as fit, make
+// one block of columns for the matrix pipe; the eight waves of a workgroup take every eighth tile of 64 keys each, by themselves: keys straight into
+// the registers that the matrix pipe reads, values through a region of LDS of the wave's own for their columns, both requested a tile ahead. No barrier
+// but for the join of the waves at the end.
+// ---------------------------------------------------------------------------
+constexpr int kFewRows = 16, kFewWaves = 8;
+
+// Where the rows of a workgroup stand: `heads` neighbouring heads of those that share keys, Lq queries each.
+struct FewPlace {
+  int heads, parts;  // of a workgroup; workgroups for the heads that share keys
+};
+
 template <int DH>
-__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, Outputs out, long Lq, int H, int nq, int rows, int slices,
-                                                        long units) {
-  constexpr int E = DH / 64;  // values of a lane
+__global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, int Lq,
+                                                                     long Lk, int H, int group, FewPlace place, int slices) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, TILE = kTileKeys * DH;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];  // [waves][TILE] values, then the waves' results; biases of each head
+  float* const s_bias = reinterpret_cast<float*>(smem + kFewWaves * TILE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 15, g = lane >> 4, Hk = H / group, width = bias.width(), far = bias.far;
+  const int unit = blockIdx.x, tile = unit / slices, slice = unit - tile * slices;
+  const int in_group = tile % place.parts, bk = tile / place.parts, b = bk / Hk, kv_head = bk - b * Hk;
+  const int head0 = kv_head * group + in_group * place.heads;
+  const int heads = group - in_group * place.heads < place.heads ? group - in_group * place.heads : place.heads;
+  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int live_rows = heads * Lq, row = lq < live_rows ? lq : live_rows - 1, of_head = row / Lq, q = row - of_head * Lq;
+  int most = n;  // keys that some query sees
+  if (bias.causal) most = origin + Lq < 0 ? 0 : origin + Lq < n ? origin + Lq : n;
+  const int steps = (most + kTileKeys - 1) / kTileKeys;
+  const int t1 = (int)((long)steps * (slice + 1) / slices);
+  int t = (int)((long)steps * slice / slices) + wave;
+
+  TileStage<DH, 64> v_in(lane, V.row);
+  const uint16_t* const k_base = K.p + (long)b * K.batch + (long)kv_head * DH;
+  const uint16_t* const v_base = V.p + (long)b * V.batch + (long)kv_head * DH;
+  const int k_bytes = (int)(K.row * 2);
+  u32x4 kf[KB][KC];
+  auto fetch_k = [&](int at) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(uniform(k_base + (long)at * kTileKeys * K.row), 0, -1, 0x00027000);
+    const int rest = n - 1 - at * kTileKeys;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int r = 16 * kb + lq;
+      const int from = (r < rest ? r : rest) * k_bytes + 16 * g;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) kf[kb][kc] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, from, 64 * kc, 0));
+    }
+  };
+  auto fetch_v = [&](int at) { v_in.fetch(v_base + (long)at * kTileKeys * V.row, n - 1 - at * kTileKeys); };
+  if (t < t1) {
+    fetch_k(t);
+    fetch_v(t);
+  }
+  bf16x8 qf[KC];
+  {
+    const uint16_t* qp = Q.p + (long)b * Q.batch + (long)q * Q.row + (long)(head0 + of_head) * DH + 8 * g;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
+  }
+  for (int i = tid; i < heads * width; i += 64 * kFewWaves) s_bias[i] = bias.bias(i % width, head0 + i / width, H);
+  lds_barrier();
+  const float* const my_bias = s_bias + of_head * width;
+  const float below = my_bias[0], above = my_bias[width - 1];
+  const float scale = bias.scale * kLog2E;
+  const ColumnFragments<DH> v_at(lane);
+  uint16_t* const v_tile = smem + wave * TILE;
+  int end = n;  // first key that this lane's query does not see
+  if (bias.causal && origin + q + 1 < end) end = origin + q + 1;
+
+  f32x4 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = 0.f, l_run = 0.f;  // reference, in powers of two, and this lane's share of the sum of the weights
+  bool seen = false;
+  for (; t < t1; t += kFewWaves) {
+    f32x4 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) s[kb] = mfma(__builtin_bit_cast(bf16x8, kf[kb][kc]), qf[kc], s[kb]);
+    }
+    v_in.store(v_tile);
+    if (t + kFewWaves < t1) {
+      fetch_k(t + kFewWaves);
+      fetch_v(t + kFewWaves);
+    }
+    const int nearest = t * kTileKeys - origin;  // distance of the tile's first key from query 0
+    if (nearest + 63 > -far && nearest - (kFewRows - 1) < far) {
+      const float* at = my_bias + (nearest - q + far + kPad + 4 * g);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i] - m_run);
+    } else {
+      const float c = (nearest > 0 ? above : below) - m_run;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, c);
+    }
+    const int left = end - t * kTileKeys - 4 * g;
+    if (__any(left < kTileKeys)) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * kb + i >= left) s[kb][i] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kb][i]);
+    if (__any(!seen || mx > 8.0f)) {  // as in the tiled kernel
+      float m = fmaxf(mx, swap_rows16(mx));
+      m = fmaxf(m, swap_halves(m));
+      const bool finite = m > -INFINITY;
+      const float up = !seen ? (finite ? m : 0.f) : fmaxf(m, 0.f);
+      const float alpha = !seen ? 1.0f : __builtin_amdgcn_exp2f(-up);
+      seen = seen || finite;
+      m_run += up;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] -= up;
+    }
+    bf16x8 pf[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][e & 3]);
+        l_run += p;
+        pf[c][e] = (bf16_t)p;
+      }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) o[db] = mfma(v_at.read(v_tile, c, db), pf[c], o[db]);
+  }
+  l_run += swap_rows16(l_run);
+  l_run += swap_halves(l_run);
+
+  // the waves' results, [wave][row][DH] and (reference, sum): put together in the order of the waves
+  lds_barrier();
+  float* const s_o = reinterpret_cast<float*>(smem);
+  float2* const s_ml = reinterpret_cast<float2*>(s_o + kFewWaves * kFewRows * (DH + 4));
+#pragma unroll
+  for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(s_o + (wave * kFewRows + lq) * (DH + 4) + 16 * db + 4 * g) = o[db];
+  if (g == 0) s_ml[wave * kFewRows + lq] = make_float2(m_run, l_run);
+  lds_barrier();
+  constexpr int PER = 64 * kFewWaves / kFewRows, E = DH / PER;  // threads of a row; values of a thread
+  const int r = tid / PER, d0 = tid % PER * E;
+  if (r >= live_rows) return;
+  float top = -INFINITY, total = 0.f, sum[E] = {};
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float2 ml = s_ml[w * kFewRows + r];
+    if (ml.y != 0.f) top = fmaxf(top, ml.x);
+  }
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const float2 ml = s_ml[w * kFewRows + r];
+    const float f = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+    total = __builtin_fmaf(f, ml.y, total);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(f, s_o[(w * kFewRows + r) * (DH + 4) + d0 + e], sum[e]);
+  }
+  if (slices > 1) {
+    float* op = part + ((long)unit * kFewRows + r) * DH + d0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) op[e] = sum[e];
+    if (d0 == 0) reinterpret_cast<float2*>(part + (long)gridDim.x * kFewRows * DH)[(long)unit * kFewRows + r] = make_float2(total == 0.f ? 0.f : top, total);
+    return;
+  }
+  const int head = head0 + r / Lq, qi = r % Lq;
+  const float inv = total == 0.f ? 0.f : 1.0f / total;
+  uint16_t* op = out.o.p + (long)b * out.o.batch + (long)qi * out.o.row + (long)head * DH + d0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) op[e] = f32_to_bf16(sum[e] * inv);
+  if (out.lse && d0 == 0) out.lse[((long)b * H + head) * Lq + qi] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+#endif
+}
+
+// Puts the slices of a row together, a wave a row: the largest reference, then the slices' results and sums by their distance from it, in
+// an order that depends on nothing but their number. FEW: rows of several heads, as bias_few_kernel has them; otherwise queries of one.
+template <int DH, bool FEW>
+__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, Outputs out, long Lq, int H, int group, int nq, FewPlace place,
+                                                        int slices, long units) {
+  constexpr int E = DH / 64, ROWS = FEW ? kFewRows : kTileQueries;  // values of a lane; rows of a unit
   const int lane = threadIdx.x & 63;
   const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const long tile = at / rows;
-  const int row = (int)(at - tile * rows);
-  const long bh = tile / nq, q = (tile - bh * nq) * rows + row;
-  if (tile >= units / slices || q >= Lq) return;
-  const long first = tile * slices * rows + row;
-  const float2 ml = lane < slices ? reinterpret_cast<const float2*>(part + units * rows * DH)[first + (long)lane * rows] : make_float2(0.f, 0.f);
+  const long tile = at / ROWS;
+  const int row = (int)(at - tile * ROWS);
+  if (tile >= units / slices) return;
+  long b, q;
+  int head;
+  if (FEW) {
+    const int Hk = H / group, in_group = (int)(tile % place.parts);
+    const long bk = tile / place.parts;
+    b = bk / Hk;
+    const int of_group = in_group * place.heads + row / (int)Lq;
+    if (row >= place.heads * (int)Lq || of_group >= group) return;
+    head = (int)(bk - b * Hk) * group + of_group;
+    q = row % (int)Lq;
+  } else {
+    const long bh = tile / nq;
+    b = bh / H;
+    head = (int)(bh - b * H);
+    q = (tile - bh * nq) * ROWS + row;
+    if (q >= Lq) return;
+  }
+  const long first = tile * slices * ROWS + row;
+  const float2 ml = lane < slices ? reinterpret_cast<const float2*>(part + units * ROWS * DH)[first + (long)lane * ROWS] : make_float2(0.f, 0.f);
   const float top = wave_max(ml.y != 0.f ? ml.x : -INFINITY);  // a slice without a key has no reference
   const float w = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
   const float total = wave_sum(w * ml.y), inv = total == 0.f ? 0.f : 1.0f / total;
   float sum[E] = {};
   for (int s = 0; s < slices; ++s) {
     const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-    const float* p = part + (first + (long)s * rows) * DH + E * lane;
+    const float* p = part + (first + (long)s * ROWS) * DH + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(ws, p[e], sum[e]);
   }
-  const long b = bh / H, head = bh - b * H, to = b * out.o.batch + q * out.o.row + head * DH + E * lane;
+  const long to = b * out.o.batch + q * out.o.row + (long)head * DH + E * lane;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float v = sum[e] * inv;
     out.o.p[to + e] = f32_to_bf16(v);
     if (out.rest) out.rest[to + e] = left_off(v);
   }
-  if (out.lse && lane == 0) out.lse[bh * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+  if (out.lse && lane == 0) out.lse[((long)b * H + head) * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }
 
 struct ForwardPlan {
+  bool few;  // a workgroup for the few queries of some heads; otherwise one for 128 queries of a head
+  FewPlace place;
   long tiles;
   int nq, slices;
   size_t bytes;
 };
-ForwardPlan forward_plan(int64_t B, int64_t H, int64_t Lq, int64_t Lk, int dh) {
-  ForwardPlan p;
-  p.nq = (int)((Lq + kTileQueries - 1) / kTileQueries);
-  p.tiles = (long)(B * H * p.nq);
-  p.slices = slices_of(p.tiles, (long)Lk);
-  p.bytes = slice_bytes(p.tiles, p.slices, dh, kTileQueries);
+// The few queries' kernel takes whole workgroups' worth of keys; slices of the keys where the workgroups would leave compute units idle (two are counted to a
+// unit), of at least two tiles for each wave.
+ForwardPlan forward_plan(const chorus_bias_attention& a, bool training) {
+  ForwardPlan p{};
+  p.few = !training && a.Lq <= kFewRows;
+  p.nq = (int)((a.Lq + kTileQueries - 1) / kTileQueries);
+  if (!p.few) {
+    p.tiles = (long)a.B * a.H * p.nq;
+    p.slices = slices_of(p.tiles, (long)a.Lk);
+    p.bytes = slice_bytes(p.tiles, p.slices, a.dh, kTileQueries);
+    return p;
+  }
+  const int group = a.H / a.Hk;
+  p.place.heads = kFewRows / (int)a.Lq < group ? kFewRows / (int)a.Lq : group;
+  // the heads' biases have to fit beside the values
+  const int room = (160 * 1024 - kFewWaves * kTileKeys * a.dh * 2) / (int)((2 * (a.far + kPad) + 1) * sizeof(float));
+  if (p.place.heads > room) p.place.heads = room;
+  p.place.parts = (group + p.place.heads - 1) / p.place.heads;
+  p.tiles = (long)a.B * a.Hk * p.place.parts;
+  const long steps = (a.Lk + kTileKeys - 1) / kTileKeys;
+  long s = p.tiles >= 256 ? 1 : (512 + p.tiles - 1) / p.tiles;
+  if (s > steps / (2 * kFewWaves)) s = steps / (2 * kFewWaves);
+  p.slices = s < 1 ? 1 : s > kMostSlices ? kMostSlices : (int)s;
+  p.bytes = slice_bytes(p.tiles, p.slices, a.dh, kFewRows);
   return p;
 }
 constexpr int64_t kMostTiles = 1 << 22;
@@ -412,7 +636,8 @@ int32_t chorus_bias_buckets(int32_t n_buckets, int32_t far, int32_t both_sides, 
 
 size_t chorus_attention_bias_workspace_bytes(const chorus_bias_attention* a) {
   if (check_bias_sizes(a) != CHORUS_OK || a->B == 0 || a->Lq == 0) return 0;
-  return forward_plan(a->B, a->H, a->Lq, a->Lk, a->dh).bytes;
+  const size_t serving = forward_plan(*a, false).bytes, training = forward_plan(*a, true).bytes;
+  return serving > training ? serving : training;
 }
 
 int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q, const uint16_t* K, const uint16_t* V, uint16_t* O, uint16_t* rest,
@@ -423,11 +648,12 @@ int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q,
   if (a->B == 0 || a->Lq == 0) return CHORUS_OK;
   if (!Q || !O || (a->Lk > 0 && (!K || !V))) return CHORUS_E_ARG;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(rest) || !aligned16(lse) || !aligned16(ws)) return CHORUS_E_ARG;
-  const ForwardPlan p = forward_plan(a->B, a->H, a->Lq, a->Lk, a->dh);
+  const ForwardPlan p = forward_plan(*a, rest != nullptr);
   if (p.bytes && (!ws || ws_bytes < p.bytes)) return CHORUS_E_WORKSPACE;
   const Rows q{Q, (long)a->q_row, (long)a->q_batch}, k{K, (long)a->k_row, (long)a->k_batch}, v{V, (long)a->v_row, (long)a->v_batch};
   const Outputs out{RowsOut{O, (long)a->o_row, (long)a->o_batch}, rest, lse};
   const long units = p.tiles * p.slices;
+  const int few_tiles = kFewWaves * kTileKeys * a->dh * 2;
   const int lds = 4 * kTileKeys * a->dh * 2 + bias.width() * 4, most = 4 * kTileKeys * a->dh * 2 + (2 * (kMostFar + kPad) + 1) * 4;
   hipStream_t s = (hipStream_t)stream;
 #define ATTEND(DH, SPLIT)                                                                                                               \
@@ -437,12 +663,25 @@ int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q,
     hipLaunchKernelGGL((bias_attention_kernel<DH, SPLIT>), dim3((unsigned)units), dim3(256), lds, s, q, k, v, out, bias, (float*)ws,           \
                        (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, p.nq, p.slices);                                                   \
     CHORUS_LAUNCH_CHECK();                                                                                                              \
-    if (p.slices > 1) {                                                                                                                 \
-      hipLaunchKernelGGL((bias_join_kernel<DH>), dim3((unsigned)((p.tiles * kTileQueries + 3) / 4)), dim3(256), 0, s, (const float*)ws, \
-                         out, (long)a->Lq, a->H, p.nq, kTileQueries, p.slices, units);                                                  \
-      CHORUS_LAUNCH_CHECK();                                                                                                            \
-    }                                                                                                                                   \
   } while (0)
+#define JOIN(DH, FEW, ROWS)                                                                                                            \
+  hipLaunchKernelGGL((bias_join_kernel<DH, FEW>), dim3((unsigned)((p.tiles * ROWS + 3) / 4)), dim3(256), 0, s, (const float*)ws, out, \
+                     (long)a->Lq, a->H, a->H / a->Hk, p.nq, p.place, p.slices, units)
+#define FEW(DH)                                                                                                                        \
+  do {                                                                                                                                 \
+    static DynLdsOnce once;                                                                                                            \
+    CHK_STATUS(once.ensure((const void*)bias_few_kernel<DH>, 160 * 1024));                                                             \
+    hipLaunchKernelGGL((bias_few_kernel<DH>), dim3((unsigned)units), dim3(64 * kFewWaves), few_tiles + p.place.heads * bias.width() * 4, s, q, k, \
+                       v, out, bias, (float*)ws, (int)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, p.place, p.slices);                      \
+    CHORUS_LAUNCH_CHECK();                                                                                                             \
+    if (p.slices > 1) JOIN(DH, true, kFewRows);                                                                                        \
+  } while (0)
+  if (p.few) {
+    if (a->dh == 128) FEW(128);
+    else FEW(64);
+    CHORUS_LAUNCH_CHECK();
+    return CHORUS_OK;
+  }
   if (a->dh == 128) {
     if (rest) ATTEND(128, true);
     else ATTEND(128, false);
@@ -450,7 +689,14 @@ int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q,
     if (rest) ATTEND(64, true);
     else ATTEND(64, false);
   }
+  if (p.slices > 1) {
+    if (a->dh == 128) JOIN(128, false, kTileQueries);
+    else JOIN(64, false, kTileQueries);
+    CHORUS_LAUNCH_CHECK();
+  }
 #undef ATTEND
+#undef FEW
+#undef JOIN
   return CHORUS_OK;
 }
 

@@ -109,6 +109,8 @@ FORWARD = [
     dict(B_=1, H=3, Hk=3, dh=128, Lq=16, Lk=2100), dict(B_=2, H=2, Hk=2, dh=128, Lq=17, Lk=1500, lens=[1500, 300], first=[700, 100]),
     dict(B_=1, H=2, Hk=2, dh=64, Lq=260, Lk=1300, first=[520], far=512, buckets=64), dict(B_=1, H=2, Hk=2, dh=64, Lq=90, Lk=90, far=3, buckets=4),
     dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[-2000000000]), dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[2000000000], far=512),
+    dict(B_=2, H=12, Hk=2, dh=128, Lq=3, Lk=2500, lens=[2500, 1100], first=[2497, 1090], causal=True, both=False), dict(B_=1, H=40, Hk=1, dh=128, Lq=1, Lk=300, far=512),
+    dict(B_=1, H=5, Hk=1, dh=64, Lq=7, Lk=4100, scale=1.0, first=[-3], far=512, buckets=64), dict(B_=5, H=64, Hk=64, dh=64, Lq=1, Lk=130, lens=[130, 0, 64, 65, 1]),
     dict(B_=2, H=8, Hk=2, dh=64, Lq=1, Lk=777, lens=[777, 401], first=[776, 400], causal=True),
 ]
 
