@@ -257,7 +257,7 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  * chorus_bias_attention
  *   B, Lq, Lk, H, Hk, dh   sequences, queries and keys of each, heads, heads of keys and values (H % Hk == 0; head h reads h / (H / Hk)); dh in {64, 128}
  *   n_buckets, far         rows of the table; distance from which on all share the bucket at the end, 0 to 512
- *   causal, scale          scale > 0, finite
+ *   causal, scale          scale from 2^-30 to 2^30
  *   *_row, *_batch         steps in values, multiples of 8; a row step at least heads * dh and at most 2^23
  * chorus_bias_buckets: host only; the usual map: bucket host [2 far + 1], the buckets of distances -far .. far. One bucket each for the
  *   nearest half of a side's buckets, near of them, then bucket near + k from the first n with (n / near)^(steps) >= (far / near)^k, steps the

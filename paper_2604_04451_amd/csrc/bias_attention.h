@@ -40,14 +40,14 @@ struct BiasArgs {
     return f < -most ? -most : f > most ? most : f;
   }
   __host__ __device__ int width() const { return 2 * (far + kPad) + 1; }  // distances that a bias or a sum is kept for, the ends repeated
-  // bias of distance i - (far + kPad), in powers of two; a bucket outside the table has none. Finite ones end at +-2^126, so that the lowest value of
-  // the type stays finite here and the difference of two biases does as well.
+  // bias of distance i - (far + kPad), in powers of two; a bucket outside the table has none. Finite ones end at +-2^90, so that the lowest value of
+  // the type, and differences of biases in units of the products, stay finite.
   __device__ __forceinline__ float bias(int i, int head, int H) const {
     int at = i - kPad;
     at = at < 0 ? 0 : at > 2 * far ? 2 * far : at;
     const int c = bucket[at];
     const float v = (unsigned)c < (unsigned)n_buckets ? table[(long)c * H + head] : 0.f;
-    return __builtin_fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2E, -0x1p126f), 0x1p126f) : v;
+    return __builtin_fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2E, -0x1p90f), 0x1p90f) : v;
   }
 };
 

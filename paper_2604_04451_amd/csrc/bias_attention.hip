@@ -36,8 +36,8 @@ struct Outputs {
 // SPLIT: for the backward pass a weight goes to the matrix pipe in two parts of 8 bits, and the other half of the result's bits goes out as well: delta =
 // dO . O then has 16 bits (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of 8 bits; SPLITCOST).
 template <int DH, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
-                                                                long Lk, int H, int group, int nq, int slices) {
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
+                                                                long Lk, int B, int H, int group, int nq, int slices) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the buffer descriptors below are types of the device compiler's alone
   constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, RB = 2, PARTS = SPLIT ? 2 : 1;
   constexpr int TILE = kTileKeys * DH;
@@ -48,7 +48,8 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
   const int lq = lane & 15, g = lane >> 4;
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
   const int tile = unit / slices, slice = unit - tile * slices;
-  const int bh = tile / nq, qb = tile - bh * nq, b = bh / H, head = bh - b * H;
+  // the sequences of a head one behind the other, so that each XCD has some of every length
+  const int hb = tile / nq, qb = tile - hb * nq, head = hb / B, b = hb - head * B;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int q0 = qb * kTileQueries + wave * 32;  // the wave's first query
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
@@ -91,10 +92,12 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
   f32x4 o[DB][RB], s[KB][RB];
   // a row's reference, in powers of two, and its lane's share of the sum of its weights
   float m_run[RB], l_run[RB];
+  f32x4 less_m[RB];  // minus the reference, in units of the products: what the sums of the matrix pipe start at
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     m_run[rb] = 0.f;
     l_run[rb] = 0.f;
+    less_m[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, at[16 * (kb - rb) + i] - m_run[rb]);
+          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, at[16 * (kb - rb) + i]);
     } else {
       const float c = nearest > 0 ? above : below;
 #pragma unroll
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, c - m_run[rb]);
+          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, c);
     }
     int end = n;  // first key that the wave's first query does not see
     if (bias.causal && origin + q0 + 1 < end) end = origin + q0 + 1;
@@ -184,6 +187,8 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
       seen[rb] = seen[rb] || finite;
       none = none || !seen[rb];
       m_run[rb] += delta;
+      const float from = -m_run[rb] / scale;
+      less_m[rb] = f32x4{from, from, from, from};
       l_run[rb] *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db][rb] *= alpha;
@@ -246,8 +251,7 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
           for (int a = 0; a < PARTS; ++a) o[db][rb] = mfma(fr[db * NC + c], pf[a][c][rb], o[db][rb]);
         } else {
           const int kb = (i - VS) / KC, at = (i - VS) % KC * 2 + u, rb = at / KC, kc = at % KC;
-          if (kc == 0) s[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-          s[kb][rb] = mfma(fr[VS + kb * KC + kc], qf[rb][kc], s[kb][rb]);
+          s[kb][rb] = mfma(fr[VS + kb * KC + kc], qf[rb][kc], kc == 0 ? less_m[rb] : s[kb][rb]);
         }
       }
       if (i + kAhead < SLOTS) read(i + kAhead);
@@ -302,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void bias_attention_kernel(Rows Q, Rows K, 
     };
     put(out.o.p, false);
     if (SPLIT) put(out.rest, true);
-    if (out.lse && g == 0 && mine < Lq) out.lse[(long)bh * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
+    if (out.lse && g == 0 && mine < Lq) out.lse[((long)b * H + head) * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
   }
 #endif
 }
@@ -498,8 +502,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
 // Puts the slices of a row together, a wave a row: the largest reference, then the slices' results and sums by their distance from it, in
 // an order that depends on nothing but their number. FEW: rows of several heads, as bias_few_kernel has them; otherwise queries of one.
 template <int DH, bool FEW>
-__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, Outputs out, long Lq, int H, int group, int nq, FewPlace place,
-                                                        int slices, long units) {
+__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, Outputs out, long Lq, int B, int H, int group, int nq,
+                                                        FewPlace place, int slices, long units) {
   constexpr int E = DH / 64, ROWS = FEW ? kFewRows : kTileQueries;  // values of a lane; rows of a unit
   const int lane = threadIdx.x & 63;
   const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -517,10 +521,10 @@ __global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict_
     head = (int)(bk - b * Hk) * group + of_group;
     q = row % (int)Lq;
   } else {
-    const long bh = tile / nq;
-    b = bh / H;
-    head = (int)(bh - b * H);
-    q = (tile - bh * nq) * ROWS + row;
+    const long hb = tile / nq;
+    head = (int)(hb / B);
+    b = hb - (long)head * B;
+    q = (tile - hb * nq) * ROWS + row;
     if (q >= Lq) return;
   }
   const long first = tile * slices * ROWS + row;
@@ -589,7 +593,7 @@ bool bias_step_ok(int64_t row, int64_t batch, int64_t heads, int32_t dh) {
 int32_t check_bias_sizes(const chorus_bias_attention* a) {
   if (!a) return CHORUS_E_ARG;
   if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->H <= 0 || a->Hk <= 0 || a->n_buckets <= 0 || a->far < 0) return CHORUS_E_ARG;
-  if (!(a->scale > 0.f) || a->scale > 3e38f) return CHORUS_E_ARG;
+  if (!(a->scale >= 0x1p-30f && a->scale <= 0x1p30f)) return CHORUS_E_ARG;
   if ((a->dh != 64 && a->dh != 128) || a->H % a->Hk || a->far > kMostFar || a->Lq > kMostTokens || a->Lk > kMostTokens) return CHORUS_E_SHAPE;
   if (a->H > (1 << 16) || a->B > (1 << 20)) return CHORUS_E_SHAPE;
   if (!bias_step_ok(a->q_row, a->q_batch, a->H, a->dh) || !bias_step_ok(a->k_row, a->k_batch, a->Hk, a->dh) || !bias_step_ok(a->v_row, a->v_batch, a->Hk, a->dh) ||
@@ -661,12 +665,12 @@ int32_t chorus_attention_bias(const chorus_bias_attention* a, const uint16_t* Q,
     static DynLdsOnce once;                                                                                                             \
     CHK_STATUS(once.ensure((const void*)bias_attention_kernel<DH, SPLIT>, most));                                                              \
     hipLaunchKernelGGL((bias_attention_kernel<DH, SPLIT>), dim3((unsigned)units), dim3(256), lds, s, q, k, v, out, bias, (float*)ws,           \
-                       (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, p.nq, p.slices);                                                   \
+                       (long)a->Lq, (long)a->Lk, a->B, a->H, a->H / a->Hk, p.nq, p.slices);                                                   \
     CHORUS_LAUNCH_CHECK();                                                                                                              \
   } while (0)
 #define JOIN(DH, FEW, ROWS)                                                                                                            \
   hipLaunchKernelGGL((bias_join_kernel<DH, FEW>), dim3((unsigned)((p.tiles * ROWS + 3) / 4)), dim3(256), 0, s, (const float*)ws, out, \
-                     (long)a->Lq, a->H, a->H / a->Hk, p.nq, p.place, p.slices, units)
+                     (long)a->Lq, a->B, a->H, a->H / a->Hk, p.nq, p.place, p.slices, units)
 #define FEW(DH)                                                                                                                        \
   do {                                                                                                                                 \
     static DynLdsOnce once;                                                                                                            \

@@ -49,7 +49,7 @@ constexpr int kWaves = 8;
 template <int DH>
 __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(Rows Q, Rows K, Rows V, Rows O, const uint16_t* __restrict__ rest, Rows dO,
                                                                                 RowsOut dQ, const float* __restrict__ lse, Delta delta, BiasArgs bias,
-                                                                                long Lq, long Lk, int H, int group, int nq) {
+                                                                                long Lq, long Lk, int B, int H, int group, int nq) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int KB = kTileKeys / 16, NC = kTileKeys / 32, KC = DH / 32, DB = DH / 16, THREADS = 64 * kWaves;
   constexpr int TILE = kTileKeys * DH;
@@ -60,7 +60,8 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   float* const s_bias = reinterpret_cast<float*>(smem + 4 * TILE);
 
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = unit / nq, qb = unit - bh * nq, b = bh / H, head = bh - b * H;
+  const int hb = unit / nq, qb = unit - hb * nq, head = hb / B, b = hb - head * B;  // as in the forward kernel
+  const long bh = (long)b * H + head;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int q0 = qb * kTileQueries + wave * 16;
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
@@ -107,7 +108,10 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     dl += swap_rows16(dl);
     dl += swap_halves(dl);
   }
-  const float ex = row_exponent(lse[(long)bh * Lq + q], live);  // exponent of the row's sum
+  // The exponent of the row's sum, in units of the products, and delta: what the sums of the matrix pipe start at.
+  const float scale = bias.scale * kLog2E;
+  const float ex = -row_exponent(lse[bh * Lq + q], live) / scale;
+  const f32x4 less_ex = {ex, ex, ex, ex}, less_dl = {-dl, -dl, -dl, -dl};
   f32x4 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -116,7 +120,6 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   lds_barrier();
   const float below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
   const float above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
-  const float scale = bias.scale * kLog2E;
 
   for (int t = 0, buf = 0; t < steps; ++t, buf ^= 1) {
     if (t + 1 < steps) store(buf ^ 1);
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     const uint16_t* const v_tile = smem + (2 + buf) * TILE;
     f32x4 s[KB], dp[KB];
     {
-      constexpr int SLOTS = KB * KC, kAhead = 4;
+      constexpr int SLOTS = KB * KC, kAhead = DH == 64 ? 2 : 4;
       bf16x8 kf[SLOTS], vf[SLOTS];
       auto read = [&](int f) {
         kf[f] = rows.read(k_tile, f / KC, f % KC);
@@ -138,13 +141,12 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
       for (int f = 0; f < SLOTS; ++f) {
         const int kb = f / KC, kc = f % KC;
         if (f + kAhead < SLOTS) read(f + kAhead);
-        if (kc == 0) s[kb] = dp[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        s[kb] = mfma(kf[f], qf[kc], s[kb]);
-        dp[kb] = mfma(vf[f], df[kc], dp[kb]);
+        s[kb] = mfma(kf[f], qf[kc], kc == 0 ? less_ex : s[kb]);
+        dp[kb] = mfma(vf[f], df[kc], kc == 0 ? less_dl : dp[kb]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    constexpr int SLOTS2 = DB * NC, kAhead2 = 4;
+    constexpr int SLOTS2 = DB * NC, kAhead2 = DH == 64 ? 3 : 4;
     bf16x8 kt[SLOTS2];
     auto read2 = [&](int f) { kt[f] = columns.read(k_tile, f % NC, f / NC); };
 #pragma unroll
@@ -156,9 +158,9 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i] - ex);
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i]);
     } else {
-      const float c = (nearest > 0 ? above : below) - ex;
+      const float c = nearest > 0 ? above : below;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float v = __builtin_amdgcn_exp2f(s[kb][i]) * (dp[kb][i] - dl);
+        const float v = __builtin_amdgcn_exp2f(s[kb][i]) * dp[kb][i];
         over += v;
         ds[kb / 2][4 * (kb % 2) + i] = (bf16_t)v;
       }
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   }
   over += swap_rows16(over);
   over += swap_halves(over);
-  if (g == 0 && live) delta.p[(long)bh * Lq + q] = dl + over;
+  if (g == 0 && live) delta.p[bh * Lq + q] = dl + over;
   const long row = q0 + (lq & 12) + g;
   put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3), row < Lq, lane);
 #endif
@@ -222,7 +224,7 @@ struct KeyShape {
 template <int DH>
 __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Rows Q, Rows K, Rows V, Rows dO, RowsOut dK, RowsOut dV,
                                                                              const float* __restrict__ lse, Delta delta, float* __restrict__ part,
-                                                                             BiasArgs bias, long Lq, long Lk, int H, int group, int nk) {
+                                                                             BiasArgs bias, long Lq, long Lk, int B, int H, int group, int nk) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef KeyShape<DH> Shape;
   constexpr int QB = 2, KC = DH / 32, DB = DH / 16, NB = Shape::kBlocks, THREADS = Shape::kThreads;
@@ -231,14 +233,14 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
                                                                    // sums of each wave, skewed rows of each
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
-  const int width = bias.width(), far = bias.far, Hk = H / group;
+  const int width = bias.width(), far = bias.far;
   float* const s_rows = reinterpret_cast<float*>(smem + 4 * TILE);
   float* const s_bias = s_rows + 4 * kTileKeys;
   float* const s_sums = s_bias + width + wave * width;
   float* const s_skew = s_bias + (1 + Shape::kWaves) * width + wave * 16 * ROW;
 
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = unit / nk, kt = unit - bh * nk, b = bh / Hk, kv_head = bh - b * Hk;
+  const int hb = unit / nk, kt = unit - hb * nk, kv_head = hb / B, b = hb - kv_head * B;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int k0 = kt * kTileQueries + wave * 16 * NB;  // the wave's first key
   const int tiles = (int)((Lq + kTileKeys - 1) / kTileKeys);
@@ -251,6 +253,7 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   const bool ragged = k0 + 16 * NB > n;  // a column behind the last key holds that key again: no gradients
 
   TileStage<DH, THREADS> q_in(tid, Q.row), d_in(tid, dO.row);
+  const float scale = bias.scale * kLog2E;
   float row_in = 0.f;
   auto fetch = [&](int head, int t) {
     q_in.fetch(Q.p + (long)b * Q.batch + (long)t * kTileKeys * Q.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
       const long q = (long)t * kTileKeys + (tid & 63);
       const bool live = q < Lq;
       const long at = ((long)b * H + head) * Lq + (live ? q : Lq - 1);
-      row_in = tid < kTileKeys ? row_exponent(lse[at], live) : delta.p[at];
+      row_in = tid < kTileKeys ? -row_exponent(lse[at], live) / scale : -delta.p[at];
     }
   };
   auto store = [&](int buf) {
@@ -291,7 +294,6 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
     }
   }
   for (int i = lane; i < 16 * ROW; i += 64) s_skew[i] = 0.f;
-  const float scale = bias.scale * kLog2E;
 
   for (int in_group = 0; in_group < group; ++in_group) {
     const int head = kv_head * group + in_group;
@@ -322,6 +324,13 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
             qf[f] = rows.read(q_tile, f / KC, f % KC);
             df[f] = rows.read(d_tile, f / KC, f % KC);
           };
+          // what the sums of the matrix pipe start at: the rows' exponents, in units of the products, and deltas
+          f32x4 less_ex[QB], less_dl[QB];
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            less_ex[qb] = *reinterpret_cast<const f32x4*>(ex + 16 * qb);
+            less_dl[qb] = *reinterpret_cast<const f32x4*>(ex + kTileKeys + 16 * qb);
+          }
 #pragma unroll
           for (int f = 0; f < kAhead; ++f) read(f);
           __builtin_amdgcn_sched_barrier(0);
@@ -331,9 +340,8 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
             if (f + kAhead < SLOTS) read(f + kAhead);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-              if (kc == 0) s[qb][nb] = dp[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-              s[qb][nb] = mfma(qf[f], kf[nb][kc], s[qb][nb]);
-              dp[qb][nb] = mfma(df[f], vf[nb][kc], dp[qb][nb]);
+              s[qb][nb] = mfma(qf[f], kf[nb][kc], kc == 0 ? less_ex[qb] : s[qb][nb]);
+              dp[qb][nb] = mfma(df[f], vf[nb][kc], kc == 0 ? less_dl[qb] : dp[qb][nb]);
             }
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -377,18 +385,16 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
         }
         bf16x8 pf[NB], ds[NB];
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(ex + 16 * qb), dl = *reinterpret_cast<const f32x4*>(ex + kTileKeys + 16 * qb);
+        for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float p = __builtin_amdgcn_exp2f(s[qb][nb][e] - x[e]);
-              s[qb][nb][e] = p * (dp[qb][nb][e] - dl[e]);
+              const float p = __builtin_amdgcn_exp2f(s[qb][nb][e]);
+              s[qb][nb][e] = p * dp[qb][nb][e];
               pf[nb][4 * qb + e] = (bf16_t)p;
               ds[nb][4 * qb + e] = (bf16_t)s[qb][nb][e];
             }
-        }
         if (ragged) {
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
@@ -564,10 +570,10 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
     CHK_STATUS(once_q.ensure((const void*)bias_dq_kernel<DH>, tiles + most_width * 4));                             \
     CHK_STATUS(once_k.ensure((const void*)bias_dkv_kernel<DH>, KeyShape<DH>::lds(most_width)));                                    \
     hipLaunchKernelGGL((bias_dq_kernel<DH>), dim3((unsigned)((long)a->B * a->H * at.nq)), dim3(64 * kWaves), lds_q, s, q, k, v, o, rest, d, gq, lse,  \
-                       delta, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nq);                                               \
+                       delta, bias, (long)a->Lq, (long)a->Lk, a->B, a->H, a->H / a->Hk, at.nq);                                               \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
     hipLaunchKernelGGL((bias_dkv_kernel<DH>), dim3((unsigned)((long)a->B * a->Hk * at.nk)), dim3(KeyShape<DH>::kThreads), KeyShape<DH>::lds(bias.width()), s, q, k, v, d, gk, gv, lse,     \
-                       delta, part, bias, (long)a->Lq, (long)a->Lk, a->H, a->H / a->Hk, at.nk);                                                     \
+                       delta, part, bias, (long)a->Lq, (long)a->Lk, a->B, a->H, a->H / a->Hk, at.nk);                                                     \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
   } while (0)
   if (a->dh == 128) BACKWARD(128);

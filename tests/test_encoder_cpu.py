@@ -79,7 +79,7 @@ def _attend(lib, a, Q=P16, K=P16, V=P16, O=P16, rest=NULL, lse=NULL, table=P16, 
 
 SHAPES = [(dict(B=-1), B.E_ARG), (dict(Lq=-1), B.E_ARG), (dict(Lk=-1), B.E_ARG), (dict(H=0), B.E_ARG), (dict(Hk=0), B.E_ARG), (dict(n_buckets=0), B.E_ARG),
           (dict(far=-1), B.E_ARG), (dict(scale=0.0), B.E_ARG), (dict(scale=-1.0), B.E_ARG), (dict(scale=float("nan")), B.E_ARG),
-          (dict(scale=float("inf")), B.E_ARG), (dict(dh=96), B.E_SHAPE), (dict(dh=32), B.E_SHAPE), (dict(Hk=3), B.E_SHAPE), (dict(far=513), B.E_SHAPE),
+          (dict(scale=float("inf")), B.E_ARG), (dict(scale=2.0 ** -31), B.E_ARG), (dict(scale=2.0 ** 31), B.E_ARG), (dict(dh=96), B.E_SHAPE), (dict(dh=32), B.E_SHAPE), (dict(Hk=3), B.E_SHAPE), (dict(far=513), B.E_SHAPE),
           (dict(Lq=(1 << 28) + 1), B.E_SHAPE), (dict(Lk=(1 << 28) + 1), B.E_SHAPE), (dict(q_row=248), B.E_SHAPE), (dict(k_row=120), B.E_SHAPE),
           (dict(v_row=132), B.E_SHAPE), (dict(o_row=(1 << 23) + 8), B.E_SHAPE), (dict(q_batch=4), B.E_SHAPE), (dict(k_batch=-8), B.E_SHAPE),
           (dict(B=1 << 20, Lq=1 << 12), B.E_SHAPE), (dict(B=1 << 20, Lk=1 << 12), B.E_SHAPE), (dict(H=1 << 17, q_row=1 << 23, o_row=1 << 23), B.E_SHAPE)]
