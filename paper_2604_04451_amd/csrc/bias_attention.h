@@ -40,14 +40,40 @@ struct BiasArgs {
     return f < -most ? -most : f > most ? most : f;
   }
   __host__ __device__ int width() const { return 2 * (far + kPad) + 1; }  // distances that a bias or a sum is kept for, the ends repeated
-  // bias of distance i - (far + kPad), in powers of two; a bucket outside the table has none. Finite ones end at +-2^90, so that the lowest value of
-  // the type, and differences of biases in units of the products, stay finite.
-  __device__ __forceinline__ float bias(int i, int head, int H) const {
-    int at = i - kPad;
-    at = at < 0 ? 0 : at > 2 * far ? 2 * far : at;
-    const int c = bucket[at];
-    const float v = (unsigned)c < (unsigned)n_buckets ? table[(long)c * H + head] : 0.f;
-    return __builtin_fabsf(v) < INFINITY ? fminf(fmaxf(v * kLog2E, -0x1p90f), 0x1p90f) : v;
+  // bucket of distance i - (far + kPad)
+  __device__ __forceinline__ int bucket_of(int i) const {
+    const int at = i - kPad;
+    return bucket[at < 0 ? 0 : at > 2 * far ? 2 * far : at];
+  }
+};
+
+// A head's biases on their way to LDS: buckets, then their values, each requested well ahead of its use. One for each distance from -(far + kPad) to far +
+// kPad, in powers of two; a bucket outside the table has none. Finite ones end at +-2^90, so that the lowest value of the type, and differences of
+// biases in units of the products, stay finite.
+template <int THREADS>
+struct BiasFill {
+  static constexpr int kEach = (2 * (kMostFar + kPad) + THREADS) / THREADS;
+  int c[kEach];
+  float v[kEach];
+  __device__ __forceinline__ void buckets(const BiasArgs& a, int tid) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      c[j] = -1;
+      if (tid + j * THREADS < a.width()) c[j] = a.bucket_of(tid + j * THREADS);
+    }
+  }
+  __device__ __forceinline__ void values(const BiasArgs& a, int head, int H) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      v[j] = 0.f;
+      if ((unsigned)c[j] < (unsigned)a.n_buckets) v[j] = a.table[(long)c[j] * H + head];
+    }
+  }
+  __device__ __forceinline__ void store(const BiasArgs& a, float* to, int tid) const {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (tid + j * THREADS < a.width())
+        to[tid + j * THREADS] = __builtin_fabsf(v[j]) < INFINITY ? fminf(fmaxf(v[j] * kLog2E, -0x1p90f), 0x1p90f) : v[j];
   }
 };
 

@@ -61,6 +61,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   const int steps = (most + kTileKeys - 1) / kTileKeys;
   const int t0 = (int)((long)steps * slice / slices), t1 = (int)((long)steps * (slice + 1) / slices);
 
+  BiasFill<256> fill;
+  fill.buckets(bias, tid);
   TileStage<DH, 256> k_in(tid, K.row), v_in(tid, V.row);
   const uint16_t* const k_base = K.p + (long)b * K.batch + (long)(head / group) * DH;
   const uint16_t* const v_base = V.p + (long)b * V.batch + (long)(head / group) * DH;
@@ -71,8 +73,6 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     fetch_v(t0);
   }
   const int width = bias.width(), far = bias.far;
-  for (int i = tid; i < width; i += 256) s_bias[i] = bias.bias(i, head, H);
-
   const RowFragments<DH> k_at(lane);
   const ColumnFragments<DH> v_at(lane);
   bf16x8 qf[RB][KC];
@@ -84,6 +84,11 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
   }
+  fill.values(bias, head, H);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) asm volatile("" : "+v"(qf[rb][kc]));  // resident before the loop, which would wait for them at every tile otherwise
   if (t0 < t1) {
     k_in.store(smem);
     v_in.store(smem + 2 * TILE);
@@ -105,6 +110,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   bool seen[RB] = {false, false};
   const float scale = bias.scale * kLog2E;
 
+  fill.store(bias, s_bias, tid);
   lds_barrier();
   const float below = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[0])));
   const float above = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s_bias[width - 1])));
@@ -130,12 +136,18 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     const int nearest = t * kTileKeys - (origin + q0);  // distance of the tile's first key from the wave's first query
     if (nearest + 63 > -far && nearest - 31 < far) {
       const float* at = s_bias + (nearest + far + kPad + 4 * g - lq);
+      f32x4 here[KB + RB - 1];
+#pragma unroll
+      for (int d = 0; d < KB + RB - 1; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) here[d][i] = at[16 * (d - RB + 1) + i];
+      __builtin_amdgcn_sched_barrier(0);  // all of them requested before the first is used
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, at[16 * (kb - rb) + i]);
+          for (int i = 0; i < 4; ++i) s[kb][rb][i] = __builtin_fmaf(s[kb][rb][i], scale, here[kb - rb + RB - 1][i]);
     } else {
       const float c = nearest > 0 ? above : below;
 #pragma unroll
@@ -233,7 +245,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     // ================= matrix phase: this tile's share of the result, and the logits of the next one =================
     // A slot is two MFMAs and the read of the fragment that is used kAhead slots on.
     __builtin_amdgcn_s_setprio(1);
-    constexpr int VS = DB * NC, SLOTS = VS + KB * KC, kAhead = 4;
+    constexpr int VS = DB * NC, SLOTS = VS + KB * KC, kAhead = DH == 64 ? 3 : 4;
     bf16x8 fr[SLOTS];
     auto read = [&](int f) {
       fr[f] = f < VS ? v_at.read(smem + (2 + buf) * TILE, f % NC, f / NC) : k_at.read(smem + (buf ^ 1) * TILE, (f - VS) / KC, (f - VS) % KC);
@@ -345,6 +357,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   const int t1 = (int)((long)steps * (slice + 1) / slices);
   int t = (int)((long)steps * slice / slices) + wave;
 
+  BiasFill<64 * kFewWaves> fill;
+  fill.buckets(bias, tid);
   TileStage<DH, 64> v_in(lane, V.row);
   const uint16_t* const k_base = K.p + (long)b * K.batch + (long)kv_head * DH;
   const uint16_t* const v_base = V.p + (long)b * V.batch + (long)kv_head * DH;
@@ -372,7 +386,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) qf[kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
   }
-  for (int i = tid; i < heads * width; i += 64 * kFewWaves) s_bias[i] = bias.bias(i % width, head0 + i / width, H);
+  for (int h = 0; h < heads; ++h) {
+    fill.values(bias, head0 + h, H);
+    fill.store(bias, s_bias + h * width, tid);
+  }
   lds_barrier();
   const float* const my_bias = s_bias + of_head * width;
   const float below = my_bias[0], above = my_bias[width - 1];
@@ -403,10 +420,16 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
     const int nearest = t * kTileKeys - origin;  // distance of the tile's first key from query 0
     if (nearest + 63 > -far && nearest - (kFewRows - 1) < far) {
       const float* at = my_bias + (nearest - q + far + kPad + 4 * g);
+      f32x4 here[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i] - m_run);
+        for (int i = 0; i < 4; ++i) here[kb][i] = at[16 * kb + i];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, here[kb][i] - m_run);
     } else {
       const float c = (nearest > 0 ? above : below) - m_run;
 #pragma unroll

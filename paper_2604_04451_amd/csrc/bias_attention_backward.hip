@@ -83,8 +83,9 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     k_in.store(smem + buf * TILE);
     v_in.store(smem + (2 + buf) * TILE);
   };
+  BiasFill<THREADS> fill;
+  fill.buckets(bias, tid);
   if (steps > 0) fetch(0);
-  for (int i = tid; i < width; i += THREADS) s_bias[i] = bias.bias(i, head, H);
 
   const RowFragments<DH> rows(lane);
   const ColumnFragments<DH> columns(lane);
@@ -96,15 +97,20 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     const uint16_t* qp = Q.p + (long)b * Q.batch + q * Q.row + (long)head * DH + 8 * g;
     const uint16_t* dp = dO.p + (long)b * dO.batch + q * dO.row + (long)head * DH + 8 * g;
     const long at = (long)b * O.batch + q * O.row + (long)head * DH + 8 * g;
+    u32x4 o[KC], r[KC];
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       qf[kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
       df[kc] = *reinterpret_cast<const bf16x8*>(dp + 32 * kc);
-      const u32x4 o = *reinterpret_cast<const u32x4*>(O.p + at + 32 * kc), r = *reinterpret_cast<const u32x4*>(rest + at + 32 * kc);
+      o[kc] = *reinterpret_cast<const u32x4*>(O.p + at + 32 * kc);
+      r[kc] = *reinterpret_cast<const u32x4*>(rest + at + 32 * kc);
+    }
+    fill.values(bias, head, H);
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        dl = __builtin_fmaf((float)df[kc][e], both_halves((uint16_t)(o[e / 2] >> 16 * (e % 2)), (uint16_t)(r[e / 2] >> 16 * (e % 2))), dl);
-    }
+        dl = __builtin_fmaf((float)df[kc][e], both_halves((uint16_t)(o[kc][e / 2] >> 16 * (e % 2)), (uint16_t)(r[kc][e / 2] >> 16 * (e % 2))), dl);
     dl += swap_rows16(dl);
     dl += swap_halves(dl);
   }
@@ -115,6 +121,9 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   f32x4 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc) asm volatile("" : "+v"(qf[kc]), "+v"(df[kc]));  // resident before the loop, which would wait for them at every tile otherwise
+  fill.store(bias, s_bias, tid);
   if (steps > 0) store(0);
   if (steps > 1) fetch(1);
   lds_barrier();
@@ -155,10 +164,16 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     const int nearest = t * kTileKeys - (origin + q0);  // distance of the tile's first key from the wave's first query
     if (nearest + 63 > -far && nearest - 15 < far) {
       const float* at = s_bias + (nearest + far + kPad + 4 * g - lq);
+      f32x4 here[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, at[16 * kb + i]);
+        for (int i = 0; i < 4; ++i) here[kb][i] = at[16 * kb + i];
+      __builtin_amdgcn_sched_barrier(0);  // all of them requested before the first is used
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, here[kb][i]);
     } else {
       const float c = nearest > 0 ? above : below;
 #pragma unroll
@@ -213,12 +228,13 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
 // it. Written ahead of the products with dS and summed behind them, so that nobody waits for what was written. A tile whose distances all
 // share an end bucket costs one addition a value.
 // ---------------------------------------------------------------------------
+constexpr int kNone = 32;
 template <int DH>
 struct KeyShape {
   static constexpr int kBlocks = DH == 64 ? 2 : 1, kWaves = 8 / kBlocks, kThreads = 64 * kWaves;  // blocks of 16 keys of a wave
   static constexpr int kDiagonals = 2 + kBlocks - 1, kPlaces = 16 * kDiagonals + 15, kRow = kPlaces + 2;  // of 32 queries
   static_assert(kPlaces <= 64, "a lane a place");
-  static int lds(int width) { return 4 * kTileKeys * DH * 2 + (4 * kTileKeys + (1 + kWaves) * width + kWaves * 16 * kRow) * 4; }
+  static int lds(int width) { return 4 * kTileKeys * DH * 2 + (4 * kTileKeys + kNone + (1 + kWaves) * width + kWaves * 16 * kRow) * 4; }
 };
 
 template <int DH>
@@ -235,7 +251,8 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   const int lq = lane & 15, g = lane >> 4;
   const int width = bias.width(), far = bias.far;
   float* const s_rows = reinterpret_cast<float*>(smem + 4 * TILE);
-  float* const s_bias = s_rows + 4 * kTileKeys;
+  float* const s_none = s_rows + 4 * kTileKeys + kNone - 1;  // the last of as many biases of -inf
+  float* const s_bias = s_none + 1;
   float* const s_sums = s_bias + width + wave * width;
   float* const s_skew = s_bias + (1 + Shape::kWaves) * width + wave * 16 * ROW;
 
@@ -250,27 +267,33 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
     first_tile = q <= 0 ? 0 : q / kTileKeys < tiles ? q / kTileKeys : tiles;
   }
   const int each = kt * kTileQueries < n ? tiles - first_tile : 0;
-  const bool ragged = k0 + 16 * NB > n;  // a column behind the last key holds that key again: no gradients
+  // a column behind the last key holds that key again, with a bias of -inf
+  bool counts[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) counts[nb] = k0 + 16 * nb + lq < n;
 
   TileStage<DH, THREADS> q_in(tid, Q.row), d_in(tid, dO.row);
-  const float scale = bias.scale * kLog2E;
+  const float scale = bias.scale * kLog2E, per_scale = 1.0f / scale;
   float row_in = 0.f;
+  bool row_live = false;
   auto fetch = [&](int head, int t) {
     q_in.fetch(Q.p + (long)b * Q.batch + (long)t * kTileKeys * Q.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
     d_in.fetch(dO.p + (long)b * dO.batch + (long)t * kTileKeys * dO.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
     if (tid < 2 * kTileKeys) {
       const long q = (long)t * kTileKeys + (tid & 63);
-      const bool live = q < Lq;
-      const long at = ((long)b * H + head) * Lq + (live ? q : Lq - 1);
-      row_in = tid < kTileKeys ? -row_exponent(lse[at], live) / scale : -delta.p[at];
+      row_live = q < Lq;
+      const long at = ((long)b * H + head) * Lq + (row_live ? q : Lq - 1);
+      row_in = *(tid < kTileKeys ? lse + at : delta.p + at);  // looked at when it is stored: here the wave would wait for it
     }
   };
   auto store = [&](int buf) {
     q_in.store(smem + buf * TILE);
     d_in.store(smem + (2 + buf) * TILE);
-    if (tid < 2 * kTileKeys) s_rows[buf * 2 * kTileKeys + tid] = row_in;
+    if (tid < 2 * kTileKeys) s_rows[buf * 2 * kTileKeys + tid] = tid < kTileKeys ? -row_exponent(row_in, row_live) * per_scale : -row_in;
   };
 
+  BiasFill<THREADS> fill;
+  fill.buckets(bias, tid);
   const RowFragments<DH> rows(lane);
   const ColumnFragments<DH> columns(lane);
   bf16x8 kf[NB][KC], vf[NB][KC];
@@ -293,13 +316,19 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
       dv[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) asm volatile("" : "+v"(kf[nb][kc]), "+v"(vf[nb][kc]));  // resident before the loop, which would wait for them at every tile otherwise
   for (int i = lane; i < 16 * ROW; i += 64) s_skew[i] = 0.f;
+  if (tid < kNone) s_none[-tid] = -INFINITY;
 
   for (int in_group = 0; in_group < group; ++in_group) {
     const int head = kv_head * group + in_group;
     if (each > 0) fetch(head, first_tile);
-    for (int i = tid; i < width; i += THREADS) s_bias[i] = bias.bias(i, head, H);
+    fill.values(bias, head, H);
     for (int i = lane; i < width; i += 64) s_sums[i] = 0.f;
+    fill.store(bias, s_bias, tid);
     if (each > 0) store(0);
     if (each > 1) fetch(head, first_tile + 1);
     lds_barrier();
@@ -358,21 +387,31 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
         const int nearest = k0 - (origin + t * kTileKeys + 32 * half);  // distance of the wave's first key from the half's first query
         const bool near = nearest + 16 * NB - 1 > -far && nearest - 31 < far;
         if (near) {
-          const float* at = s_bias + (nearest + far + kPad + lq - 4 * g);
+          f32x4 here[NB][QB];
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
+          for (int nb = 0; nb < NB; ++nb) {
+            const float* at = counts[nb] ? s_bias + (nearest + 16 * nb + far + kPad + lq - 4 * g) : s_none;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, at[16 * (nb - qb) - e]);
+              for (int e = 0; e < 4; ++e) here[nb][qb][e] = at[-16 * qb - e];
+          }
+          __builtin_amdgcn_sched_barrier(0);  // all of them requested before the first is used
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, here[nb][qb][e]);
         } else {
-          const float c = nearest > 0 ? above : below;
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
+          for (int nb = 0; nb < NB; ++nb) {
+            const float c = counts[nb] ? (nearest > 0 ? above : below) : -INFINITY;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
               for (int e = 0; e < 4; ++e) s[qb][nb][e] = __builtin_fmaf(s[qb][nb][e], scale, c);
+          }
         }
         if (bias.causal && nearest + 16 * NB - 1 > 0) {
 #pragma unroll
@@ -395,14 +434,6 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
               pf[nb][4 * qb + e] = (bf16_t)p;
               ds[nb][4 * qb + e] = (bf16_t)s[qb][nb][e];
             }
-        if (ragged) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            if (k0 + 16 * nb + lq >= n) {
-#pragma unroll
-              for (int qb = 0; qb < QB; ++qb) s[qb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-        }
         if (near) {
           float* const row = s_skew + lq * (ROW + 1) + 15 - 4 * g;
 #pragma unroll
@@ -439,10 +470,16 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
         if (near) {
           __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
           if (lane < Shape::kPlaces) {
-            float a = 0.f;
+            float a[16], *const sum = s_sums + (nearest - 31 + far + kPad + lane);
+            const float before = *sum;
 #pragma unroll
-            for (int c = 0; c < 16; ++c) a += s_skew[c * ROW + lane];
-            s_sums[nearest - 31 + far + kPad + lane] += a;
+            for (int c = 0; c < 16; ++c) a[c] = s_skew[c * ROW + lane];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n2 = 8; n2 > 0; n2 /= 2)
+#pragma unroll
+              for (int c = 0; c < n2; ++c) a[c] += a[c + n2];
+            *sum = before + a[0];
           }
           __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
         }
@@ -468,14 +505,6 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   for (int nb = 0; nb < NB; ++nb) {
     const long k = k0 + 16 * nb + (lq & 12) + g;
     const long at = (long)kv_head * DH + 8 * (lq & 3);
-    const bool counts = k0 + 16 * nb + lq < n;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dk[nb][db][e] = counts ? dk[nb][db][e] : 0.f;
-        dv[nb][db][e] = counts ? dv[nb][db][e] : 0.f;
-      }
     put_columns<DB>(dk[nb], bias.scale, dK.p + (long)b * dK.batch + k * dK.row + at, k < Lk, lane);
     put_columns<DB>(dv[nb], 1.0f, dV.p + (long)b * dV.batch + k * dV.row + at, k < Lk, lane);
   }
