@@ -126,8 +126,11 @@ int32_t launch_gated(const Call& c, long M, int F, int K, hipStream_t s) {
   return CHORUS_OK;
 }
 
+constexpr int kTile192 = kTiles;  // 256 x 192, here alone
+
 int32_t launch_gated_tile(int tile, const Call& c, long M, int F, int K, hipStream_t s) {
   switch (tile) {
+    case kTile192: return launch_gated<8, 6, 5>(c, M, F, K, s);
     case kTile256: return launch_gated<8, 8, 5>(c, M, F, K, s);
     case kTileWide: return launch_gated<4, 8, 6>(c, M, F, K, s);
     case kTile128: return launch_gated<4, 4, 5>(c, M, F, K, s);
@@ -178,75 +181,89 @@ __device__ __forceinline__ void transpose8(u32x4 (&x)[8]) {
     for (int p = 0; p < 2; ++p) x[2 * c + p] = u32x4{t[p][c], t[2 + p][c], t[4 + p][c], t[6 + p][c]};
 }
 
-// rows [R, Cn] (R rows that count) -> columns [Cn, Rp], zeros behind R; Cn % 64 == 0, Rp % 64 == 0
-__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* __restrict__ in, uint16_t* __restrict__ out, long R, int Cn, long Rp, int tiles_c,
-                                                        long tiles) {
-  const long tile = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (tile >= tiles) return;
-  const int lane = threadIdx.x & 63, a = lane >> 3, b = lane & 7;
-  const long r0 = tile / tiles_c * 64;
-  const int c0 = (int)(tile % tiles_c) * 64;
+// A transposition: rows [R, C] (R rows that count) -> columns [C, Rp], zeros behind R; C % 64 == 0, Rp % 64 == 0
+struct Turn {
+  const uint16_t* in;
+  uint16_t* out;
+  long R, Rp;
+  int C;
+  long tiles;  // Rp / 64 * C / 64, 0: none
+};
+__device__ __forceinline__ void turn_tile(const Turn& t, long tile, int lane) {
+  const int a = lane >> 3, b = lane & 7, tiles_c = t.C / 64;
+  const long r0 = tile / tiles_c * 64 + 8 * a;
+  const int c0 = (int)(tile % tiles_c) * 64 + 8 * b;
   u32x4 x[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {  // lane (a, b) reads rows 8a + i, values 8b .. 8b + 7
-    x[i] = u32x4{0, 0, 0, 0};
-    if (r0 + 8 * a + i < R) x[i] = *reinterpret_cast<const u32x4*>(in + (r0 + 8 * a + i) * Cn + c0 + 8 * b);
-  }
+  for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const u32x4*>(t.in + (r0 + i < t.R ? r0 + i : t.R - 1) * t.C + c0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (r0 + i >= t.R) x[i] = u32x4{0, 0, 0, 0};
   transpose8(x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(out + (c0 + 8 * b + i) * Rp + r0 + 8 * a) = x[i];
+  for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(t.out + (c0 + i) * t.Rp + r0) = x[i];
 }
 
+// All that the two products want laid out, in one launch: the gradients of the projections first, then W and x as columns.
+struct Slopes {
+  const uint16_t* pre;
+  const uint16_t* dH;
+  uint16_t* d;
+  uint16_t* dt;
+  long M, Mp, tiles;
+  int F;
+};
 template <int ACT>
-__global__ __launch_bounds__(256) void gated_slopes_kernel(const uint16_t* __restrict__ pre, const uint16_t* __restrict__ dH, uint16_t* __restrict__ d,
-                                                           uint16_t* __restrict__ dt, long M, int F, long Mp, int tiles_f, long tiles) {
-  const long tile = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (tile >= tiles) return;
+__global__ __launch_bounds__(256) void gated_layout_kernel(Slopes s, Turn w, Turn x) {
+  long tile = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, a = lane >> 3, b = lane & 7;
+  if (tile >= s.tiles) {
+    tile -= s.tiles;
+    if (tile < w.tiles) return turn_tile(w, tile, lane);
+    tile -= w.tiles;
+    if (tile < x.tiles) turn_tile(x, tile, lane);
+    return;
+  }
+  const int F = s.F, tiles_f = F / 64;
   const long m0 = tile / tiles_f * 64 + 8 * a;
   const int f = (int)(tile % tiles_f) * 64 + 8 * b;
-  u32x4 dg[8], du[8];
+  u32x4 h[8], dg[8], du[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {  // rows behind the last are the last one, until they are zeros
+    const long m = m0 + i < s.M ? m0 + i : s.M - 1;
+    h[i] = *reinterpret_cast<const u32x4*>(s.dH + m * F + f);
+    dg[i] = *reinterpret_cast<const u32x4*>(s.pre + m * 2 * F + f);
+    du[i] = *reinterpret_cast<const u32x4*>(s.pre + (m * 2 + 1) * F + f);
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const long m = m0 + i;
-    dg[i] = u32x4{0, 0, 0, 0};
-    du[i] = u32x4{0, 0, 0, 0};
-    if (m >= M) continue;
-    const u32x4 h = *reinterpret_cast<const u32x4*>(dH + m * F + f);
-    const u32x4 g = *reinterpret_cast<const u32x4*>(pre + m * 2 * F + f);
-    const u32x4 u = *reinterpret_cast<const u32x4*>(pre + (m * 2 + 1) * F + f);
+    const bool live = m0 + i < s.M;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float vg[2], vu[2];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const auto of = [&](uint32_t w) { return __uint_as_float(p ? w & 0xffff0000u : w << 16); };
+        const float dh = __uint_as_float(p ? h[i][e] & 0xffff0000u : h[i][e] << 16);
         float value, slope;
-        act_slope<ACT>(kept16(g[e] >> 16 * p), value, slope);
-        vg[p] = of(h[e]) * kept16(u[e] >> 16 * p) * slope;
-        vu[p] = of(h[e]) * value;
+        act_slope<ACT>(kept16(dg[i][e] >> 16 * p), value, slope);
+        vg[p] = dh * kept16(du[i][e] >> 16 * p) * slope;
+        vu[p] = dh * value;
       }
-      dg[i][e] = pack_bf16x2(vg[0], vg[1]);
-      du[i][e] = pack_bf16x2(vu[0], vu[1]);
+      dg[i][e] = live ? pack_bf16x2(vg[0], vg[1]) : 0;
+      du[i][e] = live ? pack_bf16x2(vu[0], vu[1]) : 0;
     }
-    *reinterpret_cast<u32x4*>(d + m * 2 * F + f) = dg[i];
-    *reinterpret_cast<u32x4*>(d + (m * 2 + 1) * F + f) = du[i];
+    if (live) {
+      *reinterpret_cast<u32x4*>(s.d + (m0 + i) * 2 * F + f) = dg[i];
+      *reinterpret_cast<u32x4*>(s.d + ((m0 + i) * 2 + 1) * F + f) = du[i];
+    }
   }
   transpose8(dg);
   transpose8(du);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    *reinterpret_cast<u32x4*>(dt + (long)(f + i) * Mp + m0) = dg[i];
-    *reinterpret_cast<u32x4*>(dt + (long)(F + f + i) * Mp + m0) = du[i];
+    *reinterpret_cast<u32x4*>(s.dt + (long)(f + i) * s.Mp + m0) = dg[i];
+    *reinterpret_cast<u32x4*>(s.dt + (long)(F + f + i) * s.Mp + m0) = du[i];
   }
-}
-
-int32_t launch_transpose(const uint16_t* in, uint16_t* out, long R, int Cn, long Rp, hipStream_t s) {
-  const int tiles_c = Cn / 64;
-  const long tiles = Rp / 64 * tiles_c;
-  hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)((tiles + 3) / 4)), dim3(256), 0, s, in, out, R, Cn, Rp, tiles_c, tiles);
-  CHORUS_LAUNCH_CHECK();
-  return CHORUS_OK;
 }
 
 // Where a backward pass keeps what it lays out, in bytes from the workspace's start.
@@ -284,12 +301,16 @@ int32_t chorus_gated_ffn(const uint16_t* X, const uint16_t* W, int32_t act, uint
   if (M == 0) return CHORUS_OK;
   if (!X || !W || !H || !aligned16(X) || !aligned16(W) || !aligned16(H) || !aligned16(pre)) return CHORUS_E_ARG;
   hipStream_t s = (hipStream_t)stream;
-  if (skinny_rows(M, 2L * F, K)) {
+  if (skinny_rows(M, 2L * F)) {
     const uint16_t* W2 = W + (size_t)F * K;
     if (act == CHORUS_ACT_GELU) return launch_skinny<MmaBf16, 2>(X, W, W2, (int)M, F, K, StripGated<CHORUS_ACT_GELU>{H, pre, F}, s);
     return launch_skinny<MmaBf16, 2>(X, W, W2, (int)M, F, K, StripGated<CHORUS_ACT_SILU>{H, pre, F}, s);
   }
-  const TileCut cut = gemm_tiles(M, 2 * F, K, CHORUS_EPI_GELU_BF16);
+  TileCut cut = gemm_tiles(M, 2 * F, K, CHORUS_EPI_GELU_BF16);
+  // One round of 256 x 256 tiles that leaves units without one is a round of 256 x 192 tiles where all of those have a unit (F = 10240, K = 4096, 512
+  // rows: 160 tiles 78 us, 214 of these 67; 2048 x 2560 x 4096 79 and 67, x 1024 27 and 23). In all other products of 80 (M 100 to 3000, F 1024 to 13824) the
+  // choice by the estimates was the faster or as fast.
+  if (cut.head_rows == 0 && cut.tile == kTile256 && (M + 255) / 256 * ((F + 95) / 96) <= 256) cut.tile = kTile192;
   if (cut.head_rows) CHK_STATUS(launch_gated_tile(kTile256, Call{X, W, H, pre, act}, cut.head_rows, F, K, s));
   const size_t head = (size_t)cut.head_rows;
   return launch_gated_tile(cut.tile, Call{X + head * K, W, H + head * F, pre ? pre + head * 2 * F : nullptr, act}, (long)M - cut.head_rows, F, K, s);
@@ -314,22 +335,18 @@ int32_t chorus_gated_ffn_backward(const uint16_t* X, const uint16_t* W, const ui
   uint16_t* const dt = reinterpret_cast<uint16_t*>(base + at.dt);
   uint16_t* const xt = reinterpret_cast<uint16_t*>(base + at.xt);
   uint16_t* const wt = reinterpret_cast<uint16_t*>(base + at.wt);
-  const long mp = (long)align_up((size_t)M, 64), tiles = mp / 64 * (F / 64);
-  const dim3 grid((unsigned)((tiles + 3) / 4));
+  const long mp = (long)align_up((size_t)M, 64);
+  const Slopes slopes{pre, dH, d, dt, (long)M, mp, mp / 64 * (F / 64), F};
+  const Turn w{W, wt, 2L * F, 2L * F, K, dX ? 2L * F / 64 * (K / 64) : 0}, x{X, xt, (long)M, mp, K, dW ? mp / 64 * (K / 64) : 0};
+  const dim3 grid((unsigned)((slopes.tiles + w.tiles + x.tiles + 3) / 4));
   if (act == CHORUS_ACT_GELU)
-    hipLaunchKernelGGL(gated_slopes_kernel<CHORUS_ACT_GELU>, grid, dim3(256), 0, s, pre, dH, d, dt, (long)M, F, mp, F / 64, tiles);
+    hipLaunchKernelGGL(gated_layout_kernel<CHORUS_ACT_GELU>, grid, dim3(256), 0, s, slopes, w, x);
   else
-    hipLaunchKernelGGL(gated_slopes_kernel<CHORUS_ACT_SILU>, grid, dim3(256), 0, s, pre, dH, d, dt, (long)M, F, mp, F / 64, tiles);
+    hipLaunchKernelGGL(gated_layout_kernel<CHORUS_ACT_SILU>, grid, dim3(256), 0, s, slopes, w, x);
   CHORUS_LAUNCH_CHECK();
   const GemmParts none{nullptr, 0, nullptr, 0, nullptr};
-  if (dX) {
-    CHK_STATUS(launch_transpose(W, wt, 2L * F, K, 2L * F, s));
-    CHK_STATUS(gemm_bf16_parts(d, wt, M, K, 2 * F, CHORUS_EPI_BF16, dX, nullptr, nullptr, nullptr, 1.f, none, s));
-  }
-  if (dW) {
-    CHK_STATUS(launch_transpose(X, xt, (long)M, K, mp, s));
-    CHK_STATUS(gemm_bf16_parts(dt, xt, 2L * F, K, (int)mp, dw_epilogue, dW, nullptr, nullptr, nullptr, 1.f, none, s));
-  }
+  if (dX) CHK_STATUS(gemm_bf16_parts(d, wt, M, K, 2 * F, CHORUS_EPI_BF16, dX, nullptr, nullptr, nullptr, 1.f, none, s));
+  if (dW) CHK_STATUS(gemm_bf16_parts(dt, xt, 2L * F, K, (int)mp, dw_epilogue, dW, nullptr, nullptr, nullptr, 1.f, none, s));
   return CHORUS_OK;
 }
 

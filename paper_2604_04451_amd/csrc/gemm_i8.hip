@@ -269,7 +269,7 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
   const EpiArgs ep{out, bias, gate0, gate1, scale};
   const int units = K / 2;  // a row in units of 2 bytes
   hipStream_t s = (hipStream_t)stream;
-  if (skinny_rows(M, N, units)) return launch_i8_few(x, (long)M, N, units, epilogue, ep, s);
+  if (skinny_rows(M, N)) return launch_i8_few(x, (long)M, N, units, epilogue, ep, s);
   const TileCut cut = gemm_tiles(M, N, units, epilogue);
   if (cut.head_rows) CHK_STATUS(launch_i8_tile(kTile256, x, cut.head_rows, N, units, epilogue, ep, s));
   const size_t elt = epilogue == CHORUS_EPI_F32 || epilogue == CHORUS_EPI_RESID ? 4 : 2;

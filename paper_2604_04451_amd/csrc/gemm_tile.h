@@ -330,9 +330,8 @@ template <int WBM, int WBN, class WORDS>
 __device__ __forceinline__ void gemm16_rows_out(const WORDS& words, uint16_t* out, uint16_t* cw, long m_wave0, int n_wave0, long M, int N, long ld,
                                                 int lane) {
   constexpr int E16_BF_STRIDE = e16_bf_stride<WBN>();
-  constexpr int LPR = 2 * WBN, RPI = 64 / LPR;  // read-back: LPR lanes x 16 bytes per row, RPI rows per instruction
+  constexpr int LPR = 2 * WBN;  // read-back: LPR lanes x 16 bytes per row
   const int lj = lane & 15, lg = lane >> 4;
-  const int rrow = lane / LPR, rcol = (lane % LPR) * 8;
 #pragma unroll
   for (int mp = 0; mp < WBM / 2; ++mp) {  // pairs of 16-row blocks
 #pragma unroll
@@ -342,8 +341,8 @@ __device__ __forceinline__ void gemm16_rows_out(const WORDS& words, uint16_t* ou
         *reinterpret_cast<uint2*>(cw + (16 * mh + lj) * E16_BF_STRIDE + 16 * nb + 4 * lg) = words(nb, 2 * mp + mh);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
 #pragma unroll
-    for (int it = 0; it < 32 / RPI; ++it) {
-      const int row = RPI * it + rrow;
+    for (int it = 0; it < LPR / 2; ++it) {
+      const int row = (64 * it + lane) / LPR, rcol = (64 * it + lane) % LPR * 8;
       const long m = m_wave0 + 32 * mp + row;
       const int n = n_wave0 + rcol;
       const u32x4 v = *reinterpret_cast<const u32x4*>(cw + row * E16_BF_STRIDE + rcol);

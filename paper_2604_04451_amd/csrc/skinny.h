@@ -1,14 +1,15 @@
-// Products of a few rows with large weight matrices, C = A W^T: what they take is the time to read the weights, once. A workgroup has a
-// strip of 16 rows of W (of both matrices with NB = 2) and all rows of A; its waves share out K, in pieces of 512 bytes (256 with two
-// matrices) of each row, and go on with what stands NW pieces further while the piece before is multiplied. Weights go from memory
-// straight into the registers that the matrix pipe reads: 16 rows of 64 bytes an instruction. Nothing is shared between workgroups
-// but A, which stays in the L2s; the waves' sums meet in LDS and are added in the order of the waves.
+// Products of a few rows with weight matrices, C = A W^T: what they take is the time to read the weights, once. A workgroup has a strip of 16 rows of
+// W (of both matrices with NB = 2) and all rows of A; its waves share out K, in pieces of 256 bytes of each row, and request their next piece
+// before they multiply this one. Weights go from memory straight into the registers that the matrix pipe reads, 16 rows of 64 bytes an
+// instruction. Nothing is shared between workgroups but A, which stays in the L2s; the waves' sums meet in LDS and are added in the order
+// of the waves. Loads that leave the caches alone (non-temporal) are slower where the last-level cache holds the weights from the call before
+// (20480 x 4096 37 us, so 29) and no faster where it does not.
 #pragma once
 #include "gemm_tile.h"
 
 namespace chorus {
 
-constexpr int kSkinnyRows = 64;   // most rows of A: four blocks of 16
+constexpr int kSkinnyRows = 32;  // most rows of A: two blocks of 16
 constexpr int kSkinnyWaves = 8;   // most waves of a workgroup
 
 template <class MMA, int NB, int MB, class OUT>
@@ -16,7 +17,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_
                                                                    const uint16_t* __restrict__ W2, int M, int N, int K, OUT out) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef typename MMA::Acc Acc;
-  constexpr int U = NB == 2 || MB > 1 ? 2 : 4;  // groups of 64 units (128 bytes) of a row in a piece
+  constexpr int U = 2;  // groups of 64 units (128 bytes) of a row in a piece
   extern __shared__ __attribute__((aligned(16))) uint8_t smem_raw[];
   Acc* const part = reinterpret_cast<Acc*>(smem_raw);  // [waves][NB MB][64]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_
         const int at = (g + u < groups ? g + u : groups - 1) * BK + 32 * h;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
-          p.w[u][h][nb] = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(w[nb] + at)));
+          p.w[u][h][nb] = *reinterpret_cast<const bf16x8*>(w[nb] + at);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
           p.a[u][h][mb] = bf16x8{};
@@ -91,8 +92,11 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_
 #endif
 }
 
-// Whether a product of M rows goes this way, N rows of all weight matrices, K in units of 2 bytes.
-inline bool skinny_rows(int64_t M, int64_t N, int32_t K) { return M <= 16; }
+// Whether a product of M rows goes this way, N rows of all weight matrices. The 64 x 64 tiles of the other kernels read large matrices as fast, whatever the
+// rows, and take four columns' worth of fewer workgroups where they are small. us, this kernel and 64 x 64 tiles: i8, 1 row, 1536 x 8960 7.9 / 16.4,
+// 4096 x 4096 7.1 / 9.4, 30720 x 5120 27.1 / 23.9; 16 rows 10.6 / 16.3, 7.1 / 9.4, 39 / 24; 32 rows 14.3 / 16.3, 8.1 / 9.3, 56 / 25; pairs of
+// bf16, 1 row, 20480 x 4096 29.1 / 30.9, 27648 x 5120 51 / 44; 16 rows, 5120 x 4096 14.3 / 15.3, 20480 x 4096 36 / 31; 32 rows, 5120 x 4096 18.0 / 15.1.
+inline bool skinny_rows(int64_t M, int64_t N) { return N <= (M <= 4 ? 24576 : M <= 16 ? 8192 : M <= kSkinnyRows ? 4096 : 0); }
 
 // N = rows of each weight matrix, K in units of 2 bytes.
 template <class MMA, int NB, class OUT>
@@ -101,17 +105,15 @@ int32_t launch_skinny(const uint16_t* A, const uint16_t* W, const uint16_t* W2, 
   // waves for all units at once where the strips are few, as long as each has a piece
   int waves = strips <= 1024 ? 8 : 4;
   while (waves > 1 && waves * 2 > groups) waves /= 2;
-  const int blocks = (M + 15) / 16;
 #define SKINNY(MB)                                                                                                                       \
   {                                                                                                                                      \
     auto kern = skinny_kernel<MMA, NB, MB, OUT>;                                                                                         \
     static DynLdsOnce once;                                                                                                              \
-    CHK_STATUS(once.ensure(reinterpret_cast<const void*>(kern), kSkinnyWaves* NB* MB * 1024));                                           \
+    CHK_STATUS(once.ensure(reinterpret_cast<const void*>(kern), kSkinnyWaves * NB * MB * 1024));                                           \
     hipLaunchKernelGGL(kern, dim3((unsigned)strips), dim3(64 * waves), (size_t)waves * NB * MB * 1024, s, A, W, W2, M, N, K, out);       \
   }
-  if (blocks == 1) SKINNY(1)
-  else if (blocks == 2) SKINNY(2)
-  else SKINNY(4)
+  if (M <= 16) SKINNY(1)
+  else SKINNY(2)
 #undef SKINNY
   CHORUS_LAUNCH_CHECK();
   return CHORUS_OK;
