@@ -703,32 +703,37 @@ def chorus_bias_buckets(n_buckets, far, both_sides=True, device="cuda"):
 
 
 def _heads(t, name, shape):
-    """(row step, batch step) of a bf16 tensor [B, L, heads, dh] whose heads lie one behind the other."""
-    if not t.is_cuda or t.dtype != torch.bfloat16:
+    """(row step, batch step) of a bf16 tensor [B, L, heads, dh] whose heads lie one behind the other. shape: a torch.Size."""
+    if t.dtype is not torch.bfloat16 or not t.is_cuda:
         raise TypeError(f"{name}: device tensor of bfloat16 required")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise TypeError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     batch, row, head, one = t.stride()
     n, rows, heads, dh = shape
-    if one != 1 or (heads > 1 and head != dh):
+    if one != 1 or (head != dh and heads > 1):
         raise TypeError(f"{name}: the heads of a row must lie one behind the other")
     return row if rows > 1 else heads * dh, batch if n > 1 else 0
 
 
 def _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest):
-    if Q.dim() != 4 or K.dim() != 4 or V.dim() != 4 or O.dim() != 4:
+    q, k = Q.shape, K.shape
+    if len(q) != 4 or len(k) != 4:
         raise TypeError("Q, K, V, O: [batch, rows, heads, dh] required")
-    B, Lq, H, dh = Q.shape
-    Lk, Hk = K.shape[1], K.shape[2]
-    a = BiasAttention(Lq, Lk, B, H, Hk, dh, table.shape[0], (bucket.numel() - 1) // 2, int(bool(causal)), float(scale),
-                      *_heads(Q, "Q", (B, Lq, H, dh)), *_heads(K, "K", (B, Lk, Hk, dh)), *_heads(V, "V", (B, Lk, Hk, dh)),
-                      *_heads(O, "O", (B, Lq, H, dh)))
-    _chk(table, torch.float32, "table", (table.shape[0], H))
-    _chk(bucket, torch.int32, "bucket", (2 * a.far + 1,))
-    _chk(lens, torch.int32, "lens", (B,))
-    _chk(first, torch.int32, "first", (B,))
-    _chk(lse, torch.float32, "lse", (B, H, Lq))
-    if rest is not None and _heads(rest, "rest", (B, Lq, H, dh)) != (a.o_row, a.o_batch):
+    B, Lq, H, dh = q
+    if k[0] != B or k[3] != dh:
+        raise TypeError(f"K: expected {B} sequences of heads of {dh}")
+    buckets, far = table.shape[0], bucket.shape[0] // 2
+    a = BiasAttention(Lq, k[1], B, H, k[2], dh, buckets, far, 1 if causal else 0, scale, *_heads(Q, "Q", q), *_heads(K, "K", k), *_heads(V, "V", k),
+                      *_heads(O, "O", q))
+    _chk(table, torch.float32, "table", (buckets, H))
+    _chk(bucket, torch.int32, "bucket", (2 * far + 1,))
+    if lens is not None:
+        _chk(lens, torch.int32, "lens", (B,))
+    if first is not None:
+        _chk(first, torch.int32, "first", (B,))
+    if lse is not None:
+        _chk(lse, torch.float32, "lse", (B, H, Lq))
+    if rest is not None and _heads(rest, "rest", q) != (a.o_row, a.o_batch):
         raise TypeError("rest: must be laid out as O")
     return a
 
@@ -760,10 +765,7 @@ def chorus_attention_bias_backward(Q, K, V, O, rest, lse, dO, table, bucket, dQ,
     """dQ, dK, dV (as Q, K, V, rows any distance apart) and dtable [n_buckets, H] fp32 from dO and what the forward pass left in O, rest and lse."""
     lib = load()
     a = _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest)
-    q, k = (a.B, a.Lq, a.H, a.dh), (a.B, a.Lk, a.Hk, a.dh)
-    for n, t in (("dO", dO), ("dQ", dQ), ("dK", dK), ("dV", dV)):
-        if t.dim() != 4:
-            raise TypeError(f"{n}: [batch, rows, heads, dh] required")
+    q, k = Q.shape, K.shape
     steps = BiasAttentionSteps(*_heads(dO, "dO", q), *_heads(dQ, "dQ", q), *_heads(dK, "dK", k), *_heads(dV, "dV", k))
     _chk(dtable, torch.float32, "dtable", (a.n_buckets, a.H))
     if ws is None:

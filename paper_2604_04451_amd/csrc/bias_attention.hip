@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
   const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  const int tile = unit / slices, slice = unit - tile * slices;
+  const int tile = slices > 1 ? unit / slices : unit, slice = unit - tile * slices;
   // the sequences of a head one behind the other, so that each XCD has some of every length
   const int hb = tile / nq, qb = tile - hb * nq, head = hb / B, b = hb - head * B;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     most = m < 0 ? 0 : m < n ? m : n;
   }
   const int steps = (most + kTileKeys - 1) / kTileKeys;
-  const int t0 = (int)((long)steps * slice / slices), t1 = (int)((long)steps * (slice + 1) / slices);
+  const int t0 = slices > 1 ? steps * slice / slices : 0, t1 = slices > 1 ? steps * (slice + 1) / slices : steps;  // at most 2^22 steps and 64 slices
 
   BiasFill<256> fill;
   fill.buckets(bias, tid);
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   float* const s_bias = reinterpret_cast<float*>(smem + kFewWaves * TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4, Hk = H / group, width = bias.width(), far = bias.far;
-  const int unit = blockIdx.x, tile = unit / slices, slice = unit - tile * slices;
+  const int unit = blockIdx.x, tile = slices > 1 ? unit / slices : unit, slice = unit - tile * slices;
   const int in_group = tile % place.parts, bk = tile / place.parts, b = bk / Hk, kv_head = bk - b * Hk;
   const int head0 = kv_head * group + in_group * place.heads;
   const int heads = group - in_group * place.heads < place.heads ? group - in_group * place.heads : place.heads;
@@ -354,8 +354,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   int most = n;  // keys that some query sees
   if (bias.causal) most = origin + Lq < 0 ? 0 : origin + Lq < n ? origin + Lq : n;
   const int steps = (most + kTileKeys - 1) / kTileKeys;
-  const int t1 = (int)((long)steps * (slice + 1) / slices);
-  int t = (int)((long)steps * slice / slices) + wave;
+  const int t1 = slices > 1 ? steps * (slice + 1) / slices : steps;
+  int t = (slices > 1 ? steps * slice / slices : 0) + wave;
 
   BiasFill<64 * kFewWaves> fill;
   fill.buckets(bias, tid);
