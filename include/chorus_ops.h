@@ -265,16 +265,18 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  * chorus_attention_bias
  *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
  *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
- *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass
+ *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass; without rest, of the weights
+ *               as they are rounded to bf16
  *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
- *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe.
+ *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe, with rest to 16 bits.
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
- *   dtable dev fp32 [n_buckets, H]. steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
+ *   dtable dev fp32 [n_buckets, H]. A query behind its sequence's length is one like the others: its dO has to be zeros if it is not to count.
+ *   steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
  *   ws  dev, chorus_attention_bias_backward_workspace_bytes bytes; scratch of this call alone. Outputs must not overlap inputs. B, Lq or Lk of 0:
  *   CHORUS_E_SHAPE (the forward pass accepts them).
- * Limits: Lq, Lk up to 2^28, B up to 2^20, H up to 2^16, B * H * ceil(L / 128) up to 2^22 for L = Lq, Lk (CHORUS_E_SHAPE).
+ * Limits: Lq, Lk up to 2^28, B up to 2^20, H below 2^16, B * H * ceil(L / 128) up to 2^22 for L = Lq, Lk (CHORUS_E_SHAPE).
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t Lq, Lk;
@@ -314,7 +316,7 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
  *   The gradients of the projections are rounded to bf16, the operand type of the matrix pipe.
  *   ws  dev, chorus_gated_ffn_backward_workspace_bytes(M, F, K) bytes, scratch of this call alone
  *   Outputs must not overlap inputs. M == 0: CHORUS_E_SHAPE (the forward pass accepts it and does nothing).
- * K % 64 == 0, F % 64 == 0, both at most 2^20, M at most 2^22 (CHORUS_E_SHAPE).
+ * K % 64 == 0, F % 64 == 0, both at most 2^20, M at most 2^22; backward M F + 2 F K + M K up to 2^37 (CHORUS_E_SHAPE).
  * ------------------------------------------------------------------------ */
 #define CHORUS_ACT_GELU 0
 #define CHORUS_ACT_SILU 1

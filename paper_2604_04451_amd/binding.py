@@ -672,7 +672,7 @@ def chorus_quant_rows_i8(X, codes=None, scale=None):
     _chk(scale, torch.float32, "scale", (M,))
     if codes.dim() != 2 or codes.shape[0] != M:
         raise TypeError("codes: wrong shape")
-    ld = X.stride(0) if M > 1 else max(K, X.stride(0))
+    ld = X.stride(0) if M > 1 else K
     _status("chorus_quant_rows_i8", lib.chorus_quant_rows_i8(_p(X), ld, _p(codes), _p(scale), M, K, codes.shape[1], _stream()))
     return codes, scale
 

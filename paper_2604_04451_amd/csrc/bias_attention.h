@@ -77,6 +77,31 @@ struct BiasFill {
   }
 };
 
+// Which of `n` tiles of a head and sequence a workgroup has, and which slice of it. Workgroups are dealt out to the XCDs in turn; where heads divide
+// among them, an XCD has its share of the heads for all sequences, sequence by sequence, so that it has some of every length and a compute unit
+// that takes two or three workgroups gets them of different sequences. The tiles of one head and sequence stay together.
+struct Place {
+  int b, head, tile, slice;
+};
+__device__ __forceinline__ Place place_of(int block, int blocks, int B, int H, int n, int slices) {
+  Place p{0, 0, 0, 0};
+  int at = H % 8 ? xcd_remap(block, blocks) : block / 8;
+  if (slices > 1) {
+    p.slice = at % slices;
+    at /= slices;
+  }
+  const int of = at / n;
+  p.tile = at - of * n;
+  if (H % 8) {
+    p.head = of / B;
+    p.b = of - p.head * B;
+  } else {
+    p.b = of / (H / 8);
+    p.head = block % 8 * (H / 8) + of - p.b * (H / 8);
+  }
+  return p;
+}
+
 // A tile of rows in LDS: DH values a row, its 16-byte pieces at position piece ^ swizzle(row), such that 16 rows of a piece and its
 // neighbour, which a fragment of rows takes, meet all banks, and so do 8 rows of 32 bytes, which a fragment of columns takes.
 template <int DH>

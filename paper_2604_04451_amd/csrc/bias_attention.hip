@@ -2,12 +2,16 @@
 // the keys of each sequence of a padded batch, causal or not, one query or many.
 //
 // The tiled kernel: a workgroup of four waves takes 128 queries of a head, 32 a wave in registers, and walks over the keys 64 at a time, in
-// tiles in LDS that come from the rows as a projection leaves them. S^T = K Q^T leaves a lane with the logits of one query
-// row in the order in which its weights are the operand of O^T += V^T P^T; V^T comes out of the rows of V by transposing LDS reads. The
-// step has the two phases of the kernels over whole and listed keys: the weights on the vector pipe; then this tile's share of the result and the
-// next one's logits on the matrix pipe, the next tiles on their way in registers meanwhile. One barrier a step.
-// The bias of a distance is in LDS, in powers of two, `far` and a tile's width to either side. A wave's 32 x 64 logits read it only where
-// some distance is below `far`; tiles beyond have one value, which joins the row's reference at no cost.
+// tiles in LDS that come from the rows as a projection leaves them. S^T = K Q^T leaves a lane with the logits of one query row in the order in
+// which its weights are the operand of O^T += V^T P^T; V^T comes out of the rows of V by transposing LDS reads. A step has two phases:
+// the weights on the vector pipe; then this tile's share of the result and the next one's logits on the matrix pipe, the next tiles on
+// their way in registers meanwhile. One barrier a step; two or three waves a SIMD take turns with the pipes.
+// The bias of a distance is in LDS, in powers of two, `far` and a tile's width to either side. A wave's 64 x 32 logits read it only where some
+// distance is below `far`; tiles beyond have one value. The sums of the matrix pipe start at minus the row's reference, so that a logit
+// becomes the exponent of its weight in one fma.
+// Measured: two prompts of 512 and 256 tokens, 64 heads of 64, 16.2 us; of that 7.5 before the first and behind the last step, for which the lengths, the biases
+// and the first tiles are fetched one behind the other; a step 1.1 us, bound by the vector pipe's 160 instructions and 32 exponentials for 32
+// MFMAs. Halving the rows of a workgroup changed nothing. 8191 tokens, 12 heads of 128, weights in two parts: 605 us, 910 TFLOP/s with the second parts' products.
 #include "bias_attention.h"
 
 namespace chorus {
@@ -34,7 +38,8 @@ struct Outputs {
 };
 
 // SPLIT: for the backward pass a weight goes to the matrix pipe in two parts of 8 bits, and the other half of the result's bits goes out as well: delta =
-// dO . O then has 16 bits (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of 8 bits; SPLITCOST).
+// dO . O then has 16 bits (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of
+// 8 bits; 8191 tokens, 12 heads of 128 500 to 605 us).
 template <int DH, bool SPLIT>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
                                                                 long Lk, int B, int H, int group, int nq, int slices) {
@@ -46,10 +51,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 15, g = lane >> 4;
-  const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  const int tile = slices > 1 ? unit / slices : unit, slice = unit - tile * slices;
-  // the sequences of a head one behind the other, so that each XCD has some of every length
-  const int hb = tile / nq, qb = tile - hb * nq, head = hb / B, b = hb - head * B;
+  const Place place = place_of(blockIdx.x, gridDim.x, B, H, nq, slices);
+  const int b = place.b, head = place.head, qb = place.tile, slice = place.slice, unit = ((head * B + b) * nq + qb) * slices + slice;
   const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int q0 = qb * kTileQueries + wave * 32;  // the wave's first query
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
@@ -95,13 +98,19 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     if (t0 + 1 < t1) fetch_k(t0 + 1);
   }
   f32x4 o[DB][RB], s[KB][RB];
-  // a row's reference, in powers of two, and its lane's share of the sum of its weights
+  // A row's reference, in powers of two, and the sum of its weights: in every lane, made by the matrix pipe of the rounded ones, which are what weights
+  // the values; SPLIT: of the exact ones, a lane's share
   float m_run[RB], l_run[RB];
+  f32x4 l_sum[RB];
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)1.0f;
   f32x4 less_m[RB];  // minus the reference, in units of the products: what the sums of the matrix pipe start at
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     m_run[rb] = 0.f;
     l_run[rb] = 0.f;
+    l_sum[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
     less_m[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -201,7 +210,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       m_run[rb] += delta;
       const float from = -m_run[rb] / scale;
       less_m[rb] = f32x4{from, from, from, from};
-      l_run[rb] *= alpha;
+      if (SPLIT) l_run[rb] *= alpha;
+      else l_sum[rb] *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db][rb] *= alpha;
 #pragma unroll
@@ -224,7 +234,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float p = __builtin_amdgcn_exp2f(s[2 * c + (e >> 2)][rb][e & 3]);
-          l_run[rb] += p;
+          if (SPLIT) l_run[rb] += p;
           pf[0][c][rb][e] = (bf16_t)p;
           if (SPLIT) pf[PARTS - 1][c][rb][e] = (bf16_t)(p - (float)pf[0][c][rb][e]);
         }
@@ -253,6 +263,13 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 #pragma unroll
     for (int f = 0; f < kAhead; ++f) read(f);
     __builtin_amdgcn_sched_barrier(0);
+    if (!SPLIT) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) l_sum[rb] = mfma(ones, pf[0][c][rb], l_sum[rb]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
 #pragma unroll
@@ -280,9 +297,11 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   const int row0 = q0 + (lq & 12) + g, b4 = lq & 3;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    l_run[rb] += swap_rows16(l_run[rb]);
-    l_run[rb] += swap_halves(l_run[rb]);
-    const float l = l_run[rb], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
+    if (SPLIT) {
+      l_run[rb] += swap_rows16(l_run[rb]);
+      l_run[rb] += swap_halves(l_run[rb]);
+    }
+    const float l = SPLIT ? l_run[rb] : l_sum[rb][0], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
     const long row = row0 + 16 * rb, mine = q0 + 16 * rb + lq;
     const bool live = row < Lq;
     if (slices > 1) {
@@ -618,7 +637,7 @@ int32_t check_bias_sizes(const chorus_bias_attention* a) {
   if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->H <= 0 || a->Hk <= 0 || a->n_buckets <= 0 || a->far < 0) return CHORUS_E_ARG;
   if (!(a->scale >= 0x1p-30f && a->scale <= 0x1p30f)) return CHORUS_E_ARG;
   if ((a->dh != 64 && a->dh != 128) || a->H % a->Hk || a->far > kMostFar || a->Lq > kMostTokens || a->Lk > kMostTokens) return CHORUS_E_SHAPE;
-  if (a->H > (1 << 16) || a->B > (1 << 20)) return CHORUS_E_SHAPE;
+  if (a->H >= (1 << 16) || a->B > (1 << 20)) return CHORUS_E_SHAPE;
   if (!bias_step_ok(a->q_row, a->q_batch, a->H, a->dh) || !bias_step_ok(a->k_row, a->k_batch, a->Hk, a->dh) || !bias_step_ok(a->v_row, a->v_batch, a->Hk, a->dh) ||
       !bias_step_ok(a->o_row, a->o_batch, a->H, a->dh))
     return CHORUS_E_SHAPE;

@@ -279,9 +279,9 @@ struct Layout {
   }
 };
 
-// The library's limits on sizes: tiles' bytes within 32-bit offsets, launches within 2^31 threads of tiles.
+// Limits on sizes: a tile's bytes are within the 32-bit offsets of its loads, a launch of 64 x 64 tiles, a wave each, within 2^32 threads.
 constexpr int kMostWidth = 1 << 20;
-constexpr int64_t kMostTokens = 1 << 22;
+constexpr int64_t kMostTokens = 1 << 22, kMostTiles = 1 << 25;
 
 int32_t check_gated(int64_t M, int32_t F, int32_t K, int32_t act) {
   if (M < 0 || F <= 0 || K <= 0 || (act != CHORUS_ACT_GELU && act != CHORUS_ACT_SILU)) return CHORUS_E_ARG;
@@ -338,6 +338,7 @@ int32_t chorus_gated_ffn_backward(const uint16_t* X, const uint16_t* W, const ui
   const long mp = (long)align_up((size_t)M, 64);
   const Slopes slopes{pre, dH, d, dt, (long)M, mp, mp / 64 * (F / 64), F};
   const Turn w{W, wt, 2L * F, 2L * F, K, dX ? 2L * F / 64 * (K / 64) : 0}, x{X, xt, (long)M, mp, K, dW ? mp / 64 * (K / 64) : 0};
+  if (slopes.tiles + w.tiles + x.tiles > kMostTiles) return CHORUS_E_SHAPE;
   const dim3 grid((unsigned)((slopes.tiles + w.tiles + x.tiles + 3) / 4));
   if (act == CHORUS_ACT_GELU)
     hipLaunchKernelGGL(gated_layout_kernel<CHORUS_ACT_GELU>, grid, dim3(256), 0, s, slopes, w, x);

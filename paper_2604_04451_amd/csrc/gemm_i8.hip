@@ -122,26 +122,44 @@ __global__ __launch_bounds__(256, 1) void gemm_i8_kernel(const uint16_t* __restr
   gemm16_loop<MmaI8, OneMatrix, WBM, WBN, C, false>(sums, reinterpret_cast<uint16_t*>(smem_raw), A + m0 * K, W + (long)n0 * K, OneMatrix{}, rows_a,
                                                     rows_b, K, 0, K / BK, wave, lane);
   float as[8];
-  f32x4 ws[8];
 #pragma unroll
   for (int mb = 0; mb < WBM; ++mb) {
     const long m = m0 + wm * WTM + 16 * mb + lj;
     as[mb] = a_scale[m < M ? m : M - 1];
   }
-#pragma unroll
-  for (int nb = 0; nb < WBN; ++nb) {
+  const auto scale_of = [&](int nb) {
     const int n = n0 + wn * WTN + 16 * nb + 4 * lg;
-    ws[nb] = *reinterpret_cast<const f32x4*>(w_scale + (n < N ? n : 0));
-  }
-  const auto block = [&](int nb, int mb) {
+    return *reinterpret_cast<const f32x4*>(w_scale + (n < N ? n : 0));
+  };
+  const auto scaled = [&](int nb, int mb, const f32x4& ws) {
     i32x4 of = sums[nb][mb];
     if (WBM == 8) asm volatile("" : "+v"(of));  // turned into floats here: all at once, ahead of the stores, they spilled 16 to 40 bytes a lane
     f32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)of[e] * as[mb] * ws[nb][e];
+    for (int e = 0; e < 4; ++e) v[e] = (float)of[e] * as[mb] * ws[e];
     return v;
   };
-  gemm16_finish<EPI, WBM, WBN>(block, ep, smem_raw, wave, wm, wn, m0, n0, M, N, lane);
+  if constexpr (EPI == CHORUS_EPI_F32) {
+    // a lane stores its four consecutive columns of every block
+#pragma unroll
+    for (int nb = 0; nb < WBN; ++nb) {
+      const int n = n0 + wn * WTN + 16 * nb + 4 * lg;
+      if (n >= N) continue;
+      const f32x4 ws = scale_of(nb);
+      f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+      if (ep.bias) bias = *reinterpret_cast<const f32x4*>(ep.bias + n);
+#pragma unroll
+      for (int mb = 0; mb < WBM; ++mb) {
+        const long m = m0 + wm * WTM + 16 * mb + lj;
+        if (m < M) *reinterpret_cast<f32x4*>(static_cast<float*>(ep.out) + m * N + n) = scaled(nb, mb, ws) + bias;
+      }
+    }
+  } else {
+    f32x4 ws[8];
+#pragma unroll
+    for (int nb = 0; nb < WBN; ++nb) ws[nb] = scale_of(nb);
+    gemm16_finish<EPI, WBM, WBN>([&](int nb, int mb) { return scaled(nb, mb, ws[nb]); }, ep, smem_raw, wave, wm, wn, m0, n0, M, N, lane);
+  }
 #endif
 }
 

@@ -111,6 +111,8 @@ FORWARD = [
     dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[-2000000000]), dict(B_=1, H=1, Hk=1, dh=64, Lq=300, Lk=1200, first=[2000000000], far=512),
     dict(B_=2, H=12, Hk=2, dh=128, Lq=3, Lk=2500, lens=[2500, 1100], first=[2497, 1090], causal=True, both=False), dict(B_=1, H=40, Hk=1, dh=128, Lq=1, Lk=300, far=512),
     dict(B_=1, H=5, Hk=1, dh=64, Lq=7, Lk=4100, scale=1.0, first=[-3], far=512, buckets=64), dict(B_=5, H=64, Hk=64, dh=64, Lq=1, Lk=130, lens=[130, 0, 64, 65, 1]),
+    dict(B_=3, H=8, Hk=8, dh=64, Lq=200, Lk=200, lens=[200, 77, 0]), dict(B_=1, H=16, Hk=8, dh=128, Lq=140, Lk=1500, first=[900]),
+    dict(B_=2, H=16, Hk=16, dh=64, Lq=30, Lk=700, lens=[700, 65], causal=True, first=[670, 35]),
     dict(B_=2, H=8, Hk=2, dh=64, Lq=1, Lk=777, lens=[777, 401], first=[776, 400], causal=True),
 ]
 
