@@ -270,6 +270,9 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
  *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe, with rest to 16 bits.
+ *   Biases of any size: keys behind a finite mask, the lowest value of the type included, weigh nothing beside others and alike by themselves
+ *   (products count beside a largest logit of up to 2^60). Rows whose logits are all below -80 or beyond 700 are made one by one, which is slow.
+ *   Outputs must not overlap inputs.
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
  *   dtable dev fp32 [n_buckets, H]. A query behind its sequence's length is one like the others: its dO has to be zeros if it is not to count.

@@ -11,6 +11,17 @@ constexpr int kPad = 96;           // a near tile's distances reach 63 + 31 behi
 constexpr int kMostFar = 512;  // biases and a wave's sums of every distance fit the LDS beside the tiles
 constexpr int64_t kMostTokens = 1 << 28;
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// A row's reference, or the exponent of its sum, goes into the sums of the matrix pipe, whose roundings are of its size then: 2^-14 each at this limit, in
+// powers of two. Rows beyond it, which a large finite bias is all that is left to (or a large positive one), have no weights in the loops; a wave makes them
+// by itself behind those, in fp32, taking the reference off the bias before the product is added. No reference is below kLeastReference: a row that has
+// seen only keys with a bias of -10000, or of the lowest value of the type, has lost nothing when it sees others.
+constexpr float kMostInSums = 1024.f, kLeastReference = -32.f, kLeastSum = 0x1p-90f;
+// What multiplies the products of a row: nothing is left of them beside a reference of a size that leaves nothing of them in 64 bits either. A row that has
+// nothing but biases of the lowest value of the type has all its keys alike.
+__device__ __forceinline__ float products_by(float scale, float reference) { return __builtin_fabsf(reference) < 0x1p60f ? scale : 0.f; }
+__device__ __forceinline__ bool out_of_sums(float exponent) {
+  return __builtin_fabsf(exponent) > kMostInSums && __builtin_fabsf(exponent) < INFINITY;
+}
 
 // A tensor of heads as the kernels see it: value (b, row, head, i) at p + b * batch + row * row_step + head * dh + i.
 struct Rows {
@@ -183,6 +194,57 @@ struct ColumnFragments {
       v[4 + e] = b[e];
     }
     return v;
+  }
+};
+
+// A row that is out of the sums, made by a wave: a key a lane for the logits, a value of the result (of each 64) a lane for what is weighted by them.
+template <int DH>
+struct ApartRow {
+  const uint16_t* q;      // the row
+  const uint16_t* k;      // key 0, from row to row k_row
+  long k_row;
+  const float* s_bias;    // biases in powers of two, as BiasFill leaves them
+  int nearest, far;       // distance of key 0 from the row
+  float scale;            // with log2 e
+
+  static __device__ __forceinline__ float product(const uint16_t* a, const uint16_t* b) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < DH; i += 8) {
+      const bf16x8 x = *reinterpret_cast<const bf16x8*>(a + i), y = *reinterpret_cast<const bf16x8*>(b + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf((float)x[e], (float)y[e], sum);
+    }
+    return sum;
+  }
+  // logit of key j less ref
+  __device__ __forceinline__ float logit(int j, float ref) const {
+    const int at = nearest + j + far + kPad, last = 2 * (far + kPad);
+    return __builtin_fmaf(product(q, k + (long)j * k_row), products_by(scale, ref), s_bias[at < 0 ? 0 : at < last ? at : last] - ref);
+  }
+  __device__ __forceinline__ float most(int j0, int j1, int lane) const {
+    float m = -INFINITY;
+#pragma unroll 1
+    for (int j = j0 + lane; j < j1; j += 64) m = fmaxf(m, logit(j, 0.f));
+    return wave_max(m);
+  }
+  // sum[e] = the sum over keys j0 .. j1 of weight(j) rows[j][lane + 64 e]; weight(j) is asked of lane j - j0 - 64 i
+  template <class WEIGHT>
+  static __device__ __forceinline__ void weighted(const WEIGHT& weight, const uint16_t* rows, long row_step, int j0, int j1, int lane, float (&sum)[DH / 64]) {
+#pragma unroll
+    for (int e = 0; e < DH / 64; ++e) sum[e] = 0.f;
+#pragma unroll 1
+    for (int at = j0; at < j1; at += 64) {
+      float w = 0.f;
+      if (at + lane < j1) w = weight(at + lane);
+      const int count = j1 - at < 64 ? j1 - at : 64;
+#pragma unroll 1
+      for (int j = 0; j < count; ++j) {
+        const float wj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j));
+#pragma unroll
+        for (int e = 0; e < DH / 64; ++e) sum[e] = __builtin_fmaf(wj, bf16_to_f32(rows[(long)(at + j) * row_step + lane + 64 * e]), sum[e]);
+      }
+    }
   }
 };
 

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       }
     }
   };
-  // The reference moves when a row exceeds it by more than 2^8, and to the first finite logit of a row whatever that is.
+  // The reference moves when a row exceeds it by more than 2^8, and to the first finite logit of a row, or to kLeastReference if that is less.
   auto move = [&]() {
     float mx[RB];
     bool far_up = fresh;
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       float m = fmaxf(mx[rb], swap_rows16(mx[rb]));
       m = fmaxf(m, swap_halves(m));
       const bool finite = m > -INFINITY;
-      const float delta = !seen[rb] ? (finite ? m : 0.f) : fmaxf(m, 0.f);
+      const float delta = !seen[rb] ? (finite ? fmaxf(m, kLeastReference) : 0.f) : fmaxf(m, 0.f);
       const float alpha = !seen[rb] ? 1.0f : __builtin_amdgcn_exp2f(-delta);
       seen[rb] = seen[rb] || finite;
       none = none || !seen[rb];
@@ -295,6 +295,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   // On the way out four neighbouring lanes write 64 bytes of a row: they get them from the lanes of that row.
   const auto from_lane = [](int src, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)v); };
   const int row0 = q0 + (lq & 12) + g, b4 = lq & 3;
+  uint32_t all_apart = 0;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (SPLIT) {
@@ -303,7 +304,10 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     }
     const float l = SPLIT ? l_run[rb] : l_sum[rb][0], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
     const long row = row0 + 16 * rb, mine = q0 + 16 * rb + lq;
-    const bool live = row < Lq;
+    // rows that are out of the sums: all their logits are far below the reference, or it is too large
+    const uint32_t apart = (uint32_t)__ballot(mine < Lq && seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))) & 0xffff;
+    all_apart |= apart << 16 * rb;
+    const bool live = row < Lq && !(apart >> ((lq & 12) + g) & 1), mine_live = mine < Lq && !(apart >> lq & 1);
     if (slices > 1) {
       const long at = (long)unit * kTileQueries;
       float* op = part + (at + (row - (long)qb * kTileQueries)) * DH + 4 * b4;
@@ -314,7 +318,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
         for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(from_lane(16 * b4 + (lq & 12) + g, __float_as_uint(o[db][rb][e])));
         if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
       }
-      if (g == 0 && mine < Lq)
+      if (g == 0 && mine_live)
         reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - (long)qb * kTileQueries)] = make_float2(m_run[rb], l);
       continue;
     }
@@ -337,7 +341,43 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     };
     put(out.o.p, false);
     if (SPLIT) put(out.rest, true);
-    if (out.lse && g == 0 && mine < Lq) out.lse[((long)b * H + head) * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
+    if (out.lse && g == 0 && mine_live) out.lse[((long)b * H + head) * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
+  }
+  if (__builtin_expect(all_apart != 0, 0)) {
+    // places worked out again: kept from the start they would take registers that the loop needs
+    int b2 = __builtin_amdgcn_readfirstlane(b), head2 = __builtin_amdgcn_readfirstlane(head), qb2 = __builtin_amdgcn_readfirstlane(qb), at2 = threadIdx.x & 63;
+    asm volatile("" : "+s"(b2), "+s"(head2), "+s"(qb2), "+v"(at2));
+    const uint16_t* const keys = K.p + (long)b2 * K.batch + (long)(head2 / group) * DH;
+    const uint16_t* const values = V.p + (long)b2 * V.batch + (long)(head2 / group) * DH;
+    for (uint32_t left = all_apart; left; left &= left - 1) {
+      const int r = wave * 32 + __builtin_ctz(left), q = qb2 * kTileQueries + r, see = !bias.causal || origin + q + 1 > n ? n : origin + q + 1;
+      const int j0 = t0 * kTileKeys, j1 = t1 * kTileKeys < see ? t1 * kTileKeys : see;
+      const ApartRow<DH> x{Q.p + (long)b2 * Q.batch + q * Q.row + (long)head2 * DH, keys, K.row, s_bias, -(origin + q), far, scale};
+      const float m = x.most(j0, j1, at2);
+      float sum[DH / 64], total = 0.f;
+      ApartRow<DH>::weighted([&](int j) {
+        const float w = __builtin_amdgcn_exp2f(x.logit(j, m));
+        total += w;
+        return w;
+      }, values, V.row, j0, j1, at2, sum);
+      total = wave_sum(total);
+      const long row = (long)(((head2 * B + b2) * nq + qb2) * slices + slice) * kTileQueries + r;
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) {
+        if (slices > 1) {
+          part[row * DH + at2 + 64 * e] = sum[e];
+        } else {
+          const float v = sum[e] / total;
+          const long to = (long)b2 * out.o.batch + q * out.o.row + (long)head2 * DH + at2 + 64 * e;
+          out.o.p[to] = f32_to_bf16(v);
+          if (SPLIT) out.rest[to] = left_off(v);
+        }
+      }
+      if (at2 == 0) {
+        if (slices > 1) reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[row] = make_float2(m, total);
+        else if (out.lse) out.lse[((long)b2 * H + head2) * Lq + q] = kLn2 * (m + __builtin_amdgcn_logf(total));
+      }
+    }
   }
 #endif
 }
@@ -437,24 +477,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       fetch_v(t + kFewWaves);
     }
     const int nearest = t * kTileKeys - origin;  // distance of the tile's first key from query 0
+    f32x4 here[KB];
     if (nearest + 63 > -far && nearest - (kFewRows - 1) < far) {
       const float* at = my_bias + (nearest - q + far + kPad + 4 * g);
-      f32x4 here[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) here[kb][i] = at[16 * kb + i];
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, here[kb][i] - m_run);
     } else {
-      const float c = (nearest > 0 ? above : below) - m_run;
+      const float c = nearest > 0 ? above : below;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[kb][i] = __builtin_fmaf(s[kb][i], scale, c);
+      for (int kb = 0; kb < KB; ++kb) here[kb] = f32x4{c, c, c, c};
     }
     const int left = end - t * kTileKeys - 4 * g;
     if (__any(left < kTileKeys)) {
@@ -462,14 +496,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (16 * kb + i >= left) s[kb][i] = -INFINITY;
+          if (16 * kb + i >= left) here[kb][i] = -INFINITY;
     }
-    float mx = s[0][0];
+    // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a reference that has gone far up is
+    // looked at once more.
+    const auto exponent = [&](int kb, int i, float by) { return __builtin_fmaf(s[kb][i], by, here[kb][i] - m_run); };
+#pragma unroll 1
+    for (int again = 0; again < 2; ++again) {
+      const float by = products_by(scale, m_run);
+      float mx = -INFINITY;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kb][i]);
-    if (__any(!seen || mx > 8.0f)) {  // as in the tiled kernel
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, exponent(kb, i, by));
+      if (!__any(!seen || mx > 8.0f)) break;  // as in the tiled kernel
       float m = fmaxf(mx, swap_rows16(mx));
       m = fmaxf(m, swap_halves(m));
       const bool finite = m > -INFINITY;
@@ -480,9 +520,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       l_run *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) s[kb] -= up;
     }
+    const float by = products_by(scale, m_run);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[kb][i] = exponent(kb, i, by);
     bf16x8 pf[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)

@@ -11,8 +11,12 @@
 namespace chorus {
 namespace {
 
+// What the first pass leaves the second of every row: delta, and where it is out of the sums also its reference and the logarithm of its sum by that; and
+// which rows those are, a bit a row, 16 rows a word.
 struct Delta {
-  float* p;  // [B, H, Lq]
+  float* p;  // [3][B, H, Lq]
+  long step;  // B * H * Lq
+  uint32_t* apart;  // [B, H, 8 ceil(Lq / 128)]
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -34,8 +38,10 @@ __device__ __forceinline__ void put_columns(const f32x4 (&x)[DB], float factor, 
 }
 #endif
 
-// The logarithm of a row's sum as the exponent that its weights lose; no weight is left to a row without keys or outside the matrix.
-__device__ __forceinline__ float row_exponent(float lse, bool live) { return live && lse > -INFINITY ? lse * kLog2E : INFINITY; }
+// The logarithm of a row's sum as the exponent that its weights lose; no weight is left to a row without keys, outside the matrix or out of the sums.
+__device__ __forceinline__ float row_exponent(float lse, bool live) {
+  return live && lse > -INFINITY && !out_of_sums(lse * kLog2E) ? lse * kLog2E : INFINITY;
+}
 
 // ---------------------------------------------------------------------------
 // Queries stand still: eight waves of 16 queries in registers, keys and values 64 at a time through LDS. The products S^T = K Q^T and dP^T = V dO^T leave a
@@ -116,7 +122,8 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   }
   // The exponent of the row's sum, in units of the products, and delta: what the sums of the matrix pipe start at.
   const float scale = bias.scale * kLog2E;
-  const float ex = -row_exponent(lse[bh * Lq + q], live) / scale;
+  const float row_lse = lse[bh * Lq + q], ex = -row_exponent(row_lse, live) / scale;
+  const uint32_t apart = (uint32_t)__ballot(live && out_of_sums(row_lse * kLog2E)) & 0xffff;
   const f32x4 less_ex = {ex, ex, ex, ex}, less_dl = {-dl, -dl, -dl, -dl};
   f32x4 dq[DB];
 #pragma unroll
@@ -213,9 +220,33 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   }
   over += swap_rows16(over);
   over += swap_halves(over);
-  if (g == 0 && live) delta.p[bh * Lq + q] = dl + over;
+  if (g == 0 && live && !(apart >> lq & 1)) delta.p[bh * Lq + q] = dl + over;
+  if (lane == 0) delta.apart[(bh * nq + qb) * kWaves + wave] = apart;
   const long row = q0 + (lq & 12) + g;
-  put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3), row < Lq, lane);
+  if (__builtin_expect(apart != 0, 0)) {  // rows that are out of the sums
+    for (uint32_t left = apart; left; left &= left - 1) {
+      const int r = q0 + __builtin_ctz(left), see = !bias.causal || origin + r + 1 > n ? n : origin + r + 1;
+      const uint16_t* const dp = dO.p + (long)b * dO.batch + r * dO.row + (long)head * DH;
+      const ApartRow<DH> x{Q.p + (long)b * Q.batch + r * Q.row + (long)head * DH, k_base, K.row, s_bias, -(origin + r), far, scale};
+      const float m = x.most(0, see, lane);
+      float l = 0.f, d = 0.f, sum[DH / 64];
+#pragma unroll 1
+      for (int j = lane; j < see; j += 64) {
+        const float w = __builtin_amdgcn_exp2f(x.logit(j, m));
+        l += w;
+        d = __builtin_fmaf(w, x.product(dp, v_base + (long)j * V.row), d);
+      }
+      l = wave_sum(l);
+      d = wave_sum(d) / l;
+      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j, m)) / l * (x.product(dp, v_base + (long)j * V.row) - d); }, k_base, K.row, 0, see,
+                             lane, sum);
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) dQ.p[(long)b * dQ.batch + r * dQ.row + (long)head * DH + lane + 64 * e] = f32_to_bf16(sum[e] * bias.scale);
+      if (lane < 3) delta.p[lane * delta.step + bh * Lq + r] = lane == 0 ? d : lane == 1 ? m : __builtin_amdgcn_logf(l);
+    }
+  }
+  put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3),
+                  row < Lq && !(apart >> ((lq & 12) + g) & 1), lane);
 #endif
 }
 
@@ -326,6 +357,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   for (int in_group = 0; in_group < group; ++in_group) {
     const int head = kv_head * group + in_group;
     if (each > 0) fetch(head, first_tile);
+    const int words = (int)((Lq + kTileQueries - 1) / kTileQueries) * kWaves;
+    const uint32_t* const apart = delta.apart + ((long)b * H + head) * words;
+    uint32_t some = 0;
+    for (int i = lane; i < words; i += 64) some |= apart[i];
     fill.values(bias, head, H);
     for (int i = lane; i < width; i += 64) s_sums[i] = 0.f;
     fill.store(bias, s_bias, tid);
@@ -486,6 +521,54 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
       }
       lds_barrier();
     }
+    // rows that are out of the sums: 16 of a word, a key a lane, whose four lanes share its values
+    if (__builtin_expect(each > 0 && __any(some), 0)) {
+#pragma unroll 1
+      for (int w = 0; w < words; ++w) {
+#pragma unroll 1
+        for (uint32_t left = (uint32_t)__builtin_amdgcn_readfirstlane((int)apart[w]); left; left &= left - 1) {
+          const int r = 16 * w + __builtin_ctz(left);
+          const float* const of = delta.p + ((long)b * H + head) * Lq + r;
+          const float dl = of[0], ref = of[delta.step], log_sum = of[2 * delta.step];
+          const uint16_t* const qp = Q.p + (long)b * Q.batch + r * Q.row + (long)head * DH;
+          const uint16_t* const dp = dO.p + (long)b * dO.batch + r * dO.row + (long)head * DH;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float x = 0.f, y = 0.f;
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) {
+              const bf16x8 qv = *reinterpret_cast<const bf16x8*>(qp + 32 * kc + 8 * g), dv8 = *reinterpret_cast<const bf16x8*>(dp + 32 * kc + 8 * g);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                x = __builtin_fmaf((float)qv[e], (float)kf[nb][kc][e], x);
+                y = __builtin_fmaf((float)dv8[e], (float)vf[nb][kc][e], y);
+              }
+            }
+            x += swap_rows16(x);
+            x += swap_halves(x);
+            y += swap_rows16(y);
+            y += swap_halves(y);
+            const int dist = k0 + 16 * nb + lq - (origin + r), at = dist + far + kPad;
+            const bool sees = counts[nb] && !(bias.causal && dist > 0);
+            const float bias_here = s_bias[at < 0 ? 0 : at < width ? at : width - 1];
+            const float pw = sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(x, products_by(scale, ref), bias_here - ref) - log_sum) : 0.f;
+            const float dsw = sees ? pw * (y - dl) : 0.f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                dv[nb][db][e] = __builtin_fmaf(pw, bf16_to_f32(dp[16 * db + 4 * g + e]), dv[nb][db][e]);
+                dk[nb][db][e] = __builtin_fmaf(dsw, bf16_to_f32(qp[16 * db + 4 * g + e]), dk[nb][db][e]);
+              }
+            if (g == 0) {  // 16 distances, each of one lane
+              if (at < 0) sum_below += dsw;
+              else if (at >= width) sum_above += dsw;
+              else s_sums[at] += dsw;
+            }
+          }
+        }
+      }
+    }
     sum_below = wave_sum(sum_below);
     sum_above = wave_sum(sum_above);
     if (lane == 0) {
@@ -543,13 +626,14 @@ __global__ __launch_bounds__(256) void bias_dtable_kernel(const double* __restri
 }
 
 struct BackwardLayout {
-  size_t delta, part, sums, all;
+  size_t delta, apart, part, sums, all;
   int nq, nk;
   explicit BackwardLayout(const chorus_bias_attention& a) {
     nq = (int)((a.Lq + kTileQueries - 1) / kTileQueries);
     nk = (int)((a.Lk + kTileQueries - 1) / kTileQueries);
     delta = 0;
-    part = align_up((size_t)a.B * a.H * (size_t)a.Lq * sizeof(float), 256);
+    apart = align_up((size_t)a.B * a.H * (size_t)a.Lq * 3 * sizeof(float), 256);
+    part = apart + align_up((size_t)a.B * a.H * nq * kWaves * sizeof(uint32_t), 256);
     const size_t width = (size_t)(2 * (a.far + kPad) + 1);
     sums = part + align_up((size_t)a.B * a.H * nk * width * sizeof(float), 256);
     all = sums + (size_t)a.H * width * sizeof(double);
@@ -588,7 +672,8 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
   const Rows o{O, (long)a->o_row, (long)a->o_batch}, d{dO, (long)steps->do_row, (long)steps->do_batch};
   const RowsOut gq{dQ, (long)steps->dq_row, (long)steps->dq_batch}, gk{dK, (long)steps->dk_row, (long)steps->dk_batch},
       gv{dV, (long)steps->dv_row, (long)steps->dv_batch};
-  const Delta delta{reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.delta)};
+  const Delta delta{reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.delta), (long)a->B * a->H * (long)a->Lq,
+                    reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + at.apart)};
   float* const part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + at.part);
   const int tiles = 4 * kTileKeys * a->dh * 2, most_width = 2 * (kMostFar + kPad) + 1;
   const int lds_q = tiles + bias.width() * 4;
