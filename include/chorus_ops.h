@@ -240,7 +240,7 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
  * chorus_gemm_i8: out = epilogue((sum_k A[m][k] W[n][k]) * a_scale[m] * w_scale[n] + bias[n])
  *   A dev int8 [M, K], W dev int8 [N, K], a_scale dev fp32 [M], w_scale dev fp32 [N]; any codes, -128 included. The sums are exact.
  *   epilogue, out, bias, gate0, gate1, scale: as chorus_gemm_bf16
- *   K % 128 == 0, K <= 131072, N % 8 == 0 (CHORUS_E_SHAPE); M >= 0 arbitrary.
+ *   K % 128 == 0, K < 131072, N % 8 == 0, N <= 2^24 (CHORUS_E_SHAPE); M >= 0 arbitrary.
  * ------------------------------------------------------------------------ */
 int32_t chorus_quant_rows_i8(const uint16_t* X, int64_t ld, int8_t* out, float* scale, int64_t M, int32_t K, int32_t Kp, void* stream);
 int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int64_t M, int32_t N, int32_t K,
@@ -258,7 +258,8 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *   B, Lq, Lk, H, Hk, dh   sequences, queries and keys of each, heads, heads of keys and values (H % Hk == 0; head h reads h / (H / Hk)); dh in {64, 128}
  *   n_buckets, far         rows of the table; distance from which on all share the bucket at the end, 0 to 512
  *   causal, scale          scale from 2^-30 to 2^30
- *   *_row, *_batch         steps in values, multiples of 8; a row step at least heads * dh and at most 2^23
+ *   *_row, *_batch         steps in values, multiples of 8; a row step at least heads * dh and at most 2^23; a batch step of 0 (one sequence for all) for
+ *                          inputs only
  * chorus_bias_buckets: host only; the usual map: bucket host [2 far + 1], the buckets of distances -far .. far. One bucket each for the
  *   nearest half of a side's buckets, near of them, then bucket near + k from the first n with (n / near)^(steps) >= (far / near)^k, steps the
  *   other half. both_sides: the second half of all buckets is for keys ahead of the query (n_buckets even); otherwise those share bucket 0.
@@ -279,7 +280,7 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  *   steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
  *   ws  dev, chorus_attention_bias_backward_workspace_bytes bytes; scratch of this call alone. Outputs must not overlap inputs. B, Lq or Lk of 0:
  *   CHORUS_E_SHAPE (the forward pass accepts them).
- * Limits: Lq, Lk up to 2^28, B up to 2^20, H below 2^16, B * H * ceil(L / 128) up to 2^22 for L = Lq, Lk (CHORUS_E_SHAPE).
+ * Limits: Lq, Lk up to 2^28, B up to 2^20, H below 2^16, n_buckets up to 2^16, B * H * ceil(L / 128) up to 2^22 for L = Lq, Lk (CHORUS_E_SHAPE).
  * ------------------------------------------------------------------------ */
 typedef struct {
   int64_t Lq, Lk;

@@ -680,9 +680,9 @@ int32_t check_bias_sizes(const chorus_bias_attention* a) {
   if (a->B < 0 || a->Lq < 0 || a->Lk < 0 || a->H <= 0 || a->Hk <= 0 || a->n_buckets <= 0 || a->far < 0) return CHORUS_E_ARG;
   if (!(a->scale >= 0x1p-30f && a->scale <= 0x1p30f)) return CHORUS_E_ARG;
   if ((a->dh != 64 && a->dh != 128) || a->H % a->Hk || a->far > kMostFar || a->Lq > kMostTokens || a->Lk > kMostTokens) return CHORUS_E_SHAPE;
-  if (a->H >= (1 << 16) || a->B > (1 << 20)) return CHORUS_E_SHAPE;
+  if (a->H >= (1 << 16) || a->B > (1 << 20) || a->n_buckets > (1 << 16)) return CHORUS_E_SHAPE;
   if (!bias_step_ok(a->q_row, a->q_batch, a->H, a->dh) || !bias_step_ok(a->k_row, a->k_batch, a->Hk, a->dh) || !bias_step_ok(a->v_row, a->v_batch, a->Hk, a->dh) ||
-      !bias_step_ok(a->o_row, a->o_batch, a->H, a->dh))
+      !bias_step_ok(a->o_row, a->o_batch, a->H, a->dh) || (a->B > 1 && a->o_batch == 0))
     return CHORUS_E_SHAPE;
   const int64_t nq = (a->Lq + kTileQueries - 1) / kTileQueries, nk = (a->Lk + kTileQueries - 1) / kTileQueries;
   if (nq * a->H > kMostTiles || nk * a->H > kMostTiles || nq * a->H * a->B > kMostTiles || nk * a->H * a->B > kMostTiles) return CHORUS_E_SHAPE;

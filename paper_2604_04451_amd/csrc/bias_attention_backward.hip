@@ -661,6 +661,7 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
   if (!bias_step_ok(steps->do_row, steps->do_batch, a->H, a->dh) || !bias_step_ok(steps->dq_row, steps->dq_batch, a->H, a->dh) ||
       !bias_step_ok(steps->dk_row, steps->dk_batch, a->Hk, a->dh) || !bias_step_ok(steps->dv_row, steps->dv_batch, a->Hk, a->dh))
     return CHORUS_E_SHAPE;
+  if (a->B > 1 && (steps->dq_batch == 0 || steps->dk_batch == 0 || steps->dv_batch == 0)) return CHORUS_E_SHAPE;
   if (a->B == 0 || a->Lq == 0 || a->Lk == 0) return CHORUS_E_SHAPE;
   if (!Q || !K || !V || !O || !rest || !lse || !dO || !dQ || !dK || !dV || !dtable) return CHORUS_E_ARG;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(rest) || !aligned16(lse) || !aligned16(dO) || !aligned16(dQ) ||

@@ -11,7 +11,8 @@ namespace chorus {
 namespace {
 
 constexpr int kStep = 128;              // values of a k-step: the 128 bytes that 64 of bf16 take
-constexpr int kMostK = 131072;          // 127 * 127 * K stays below 2^31
+constexpr int kMostK = 131072 - kStep;  // 128 * 128 * K stays below 2^31
+constexpr int kMostN = 1 << 24;         // sums of tiles and columns stay within 32 bits
 constexpr float kTiny = 0x1p-100f, kHuge = 0x1p100f;
 
 // ---------------------------------------------------------------------------
@@ -277,7 +278,7 @@ int32_t chorus_quant_rows_i8(const uint16_t* X, int64_t ld, int8_t* out, float* 
 int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int64_t M, int32_t N, int32_t K,
                        int32_t epilogue, void* out, const float* bias, const float* gate0, const float* gate1, float scale, void* stream) {
   if (M < 0 || N <= 0 || K <= 0 || epilogue < CHORUS_EPI_BF16 || epilogue > CHORUS_EPI_RESID) return CHORUS_E_ARG;
-  if (K % kStep || N % 8 || K > kMostK) return CHORUS_E_SHAPE;
+  if (K % kStep || N % 8 || K > kMostK || N > kMostN) return CHORUS_E_SHAPE;
   if (M == 0) return CHORUS_OK;
   if (!A || !a_scale || !W || !w_scale || !out) return CHORUS_E_ARG;
   if (!aligned16(A) || !aligned16(a_scale) || !aligned16(W) || !aligned16(w_scale) || !aligned16(out) || !aligned16(bias) || !aligned16(gate0) ||

@@ -144,9 +144,9 @@ def test_large_tiles_and_cut_rows(M, N):
 
 
 def test_largest_sums():
-    """All codes -128 and 127 over the longest rows: 128 * 128 * 131072 is 2^31, one sign at a time stays inside."""
-    K = 131072
-    for x, y in ((127, 127), (-127, 127), (-128, 127)):
+    """All codes -128 and 127 over the longest rows that the call takes: 128 * 128 * 131072 would be 2^31."""
+    K = 131072 - 128
+    for x, y in ((127, 127), (-127, 127), (-128, 127), (-128, -128)):
         for M in (3, 70):
             a, w = np.full((M, K), x, np.int8), np.full((16, K), y, np.int8)
             _check(a, w, np.full(M, 1e-4, np.float32), np.full(16, 1e-4, np.float32), None, B.EPI_F32)
