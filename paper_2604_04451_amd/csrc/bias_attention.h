@@ -110,6 +110,11 @@ __device__ __forceinline__ Place place_of(int block, int blocks, int B, int H, i
     p.b = of / (H / 8);
     p.head = block % 8 * (H / 8) + of - p.b * (H / 8);
   }
+  // in scalar registers, where divisions do not leave them
+  p.b = __builtin_amdgcn_readfirstlane(p.b);
+  p.head = __builtin_amdgcn_readfirstlane(p.head);
+  p.tile = __builtin_amdgcn_readfirstlane(p.tile);
+  p.slice = __builtin_amdgcn_readfirstlane(p.slice);
   return p;
 }
 

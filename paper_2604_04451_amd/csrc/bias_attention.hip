@@ -81,8 +81,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   bf16x8 qf[RB][KC];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    long q = q0 + 16 * rb + lq;
-    if (q > Lq - 1) q = Lq - 1;
+    int q = q0 + 16 * rb + lq;
+    if (q > (int)Lq - 1) q = (int)Lq - 1;
     const uint16_t* qp = Q.p + (long)b * Q.batch + q * Q.row + (long)head * DH + 8 * g;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) qf[rb][kc] = *reinterpret_cast<const bf16x8*>(qp + 32 * kc);
@@ -303,14 +303,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       l_run[rb] += swap_halves(l_run[rb]);
     }
     const float l = SPLIT ? l_run[rb] : l_sum[rb][0], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
-    const long row = row0 + 16 * rb, mine = q0 + 16 * rb + lq;
+    const int row = row0 + 16 * rb, mine = q0 + 16 * rb + lq, count = (int)Lq;
     // rows that are out of the sums: all their logits are far below the reference, or it is too large
-    const uint32_t apart = (uint32_t)__ballot(mine < Lq && seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))) & 0xffff;
+    const uint32_t apart = (uint32_t)__ballot(mine < count && seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))) & 0xffff;
     all_apart |= apart << 16 * rb;
-    const bool live = row < Lq && !(apart >> ((lq & 12) + g) & 1), mine_live = mine < Lq && !(apart >> lq & 1);
+    const bool live = row < count && !(apart >> ((lq & 12) + g) & 1), mine_live = mine < count && !(apart >> lq & 1);
     if (slices > 1) {
       const long at = (long)unit * kTileQueries;
-      float* op = part + (at + (row - (long)qb * kTileQueries)) * DH + 4 * b4;
+      float* op = part + (at + (row - qb * kTileQueries)) * DH + 4 * b4;
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         f32x4 v;
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
         if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
       }
       if (g == 0 && mine_live)
-        reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - (long)qb * kTileQueries)] = make_float2(m_run[rb], l);
+        reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - qb * kTileQueries)] = make_float2(m_run[rb], l);
       continue;
     }
     const long to = (long)b * out.o.batch + row * out.o.row + (long)head * DH + 8 * b4;

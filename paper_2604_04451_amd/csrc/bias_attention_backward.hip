@@ -96,8 +96,8 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   const RowFragments<DH> rows(lane);
   const ColumnFragments<DH> columns(lane);
   bf16x8 qf[KC], df[KC];
-  const bool live = q0 + lq < Lq;
-  const long q = live ? q0 + lq : Lq - 1;
+  const bool live = q0 + lq < (int)Lq;
+  const int q = live ? q0 + lq : (int)Lq - 1;
   float dl = 0.f, over = 0.f;  // delta; what the row's gradients add up to, this lane's share
   {
     const uint16_t* qp = Q.p + (long)b * Q.batch + q * Q.row + (long)head * DH + 8 * g;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   over += swap_halves(over);
   if (g == 0 && live && !(apart >> lq & 1)) delta.p[bh * Lq + q] = dl + over;
   if (lane == 0) delta.apart[(bh * nq + qb) * kWaves + wave] = apart;
-  const long row = q0 + (lq & 12) + g;
+  const int row = q0 + (lq & 12) + g;
   if (__builtin_expect(apart != 0, 0)) {  // rows that are out of the sums
     for (uint32_t left = apart; left; left &= left - 1) {
       const int r = q0 + __builtin_ctz(left), see = !bias.causal || origin + r + 1 > n ? n : origin + r + 1;
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     }
   }
   put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3),
-                  row < Lq && !(apart >> ((lq & 12) + g) & 1), lane);
+                  row < (int)Lq && !(apart >> ((lq & 12) + g) & 1), lane);
 #endif
 }
 
@@ -310,17 +310,17 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   auto fetch = [&](int head, int t) {
     q_in.fetch(Q.p + (long)b * Q.batch + (long)t * kTileKeys * Q.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
     d_in.fetch(dO.p + (long)b * dO.batch + (long)t * kTileKeys * dO.row + (long)head * DH, (int)(Lq - 1) - t * kTileKeys);
-    if (tid < 2 * kTileKeys) {
-      const long q = (long)t * kTileKeys + (tid & 63);
-      row_live = q < Lq;
-      const long at = ((long)b * H + head) * Lq + (row_live ? q : Lq - 1);
-      row_in = *(tid < kTileKeys ? lse + at : delta.p + at);  // looked at when it is stored: here the wave would wait for it
+    if (wave < 2) {
+      const float* const from = (wave == 0 ? lse : delta.p) + ((long)b * H + head) * Lq;
+      const int q = t * kTileKeys + lane;
+      row_live = q < (int)Lq;
+      row_in = from[row_live ? q : (int)Lq - 1];  // looked at when it is stored: here the wave would wait for it
     }
   };
   auto store = [&](int buf) {
     q_in.store(smem + buf * TILE);
     d_in.store(smem + (2 + buf) * TILE);
-    if (tid < 2 * kTileKeys) s_rows[buf * 2 * kTileKeys + tid] = tid < kTileKeys ? -row_exponent(row_in, row_live) * per_scale : -row_in;
+    if (wave < 2) s_rows[buf * 2 * kTileKeys + tid] = wave == 0 ? -row_exponent(row_in, row_live) * per_scale : -row_in;
   };
 
   BiasFill<THREADS> fill;
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   f32x4 dk[NB][DB], dv[NB][DB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    long k = k0 + 16 * nb + lq;
+    int k = k0 + 16 * nb + lq;
     if (k > n - 1) k = n - 1;
     if (k < 0) k = 0;  // no keys at all: nothing is made of what is read
     const uint16_t* kp = K.p + (long)b * K.batch + k * K.row + (long)kv_head * DH + 8 * g;
@@ -357,10 +357,6 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   for (int in_group = 0; in_group < group; ++in_group) {
     const int head = kv_head * group + in_group;
     if (each > 0) fetch(head, first_tile);
-    const int words = (int)((Lq + kTileQueries - 1) / kTileQueries) * kWaves;
-    const uint32_t* const apart = delta.apart + ((long)b * H + head) * words;
-    uint32_t some = 0;
-    for (int i = lane; i < words; i += 64) some |= apart[i];
     fill.values(bias, head, H);
     for (int i = lane; i < width; i += 64) s_sums[i] = 0.f;
     fill.store(bias, s_bias, tid);
@@ -522,6 +518,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
       lds_barrier();
     }
     // rows that are out of the sums: 16 of a word, a key a lane, whose four lanes share its values
+    const int words = (int)((Lq + kTileQueries - 1) / kTileQueries) * kWaves;
+    const uint32_t* const apart = delta.apart + ((long)b * H + head) * words;
+    uint32_t some = 0;
+    for (int i = lane; i < words; i += 64) some |= apart[i];
     if (__builtin_expect(each > 0 && __any(some), 0)) {
 #pragma unroll 1
       for (int w = 0; w < words; ++w) {
@@ -586,10 +586,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
-    const long k = k0 + 16 * nb + (lq & 12) + g;
+    const int k = k0 + 16 * nb + (lq & 12) + g;
     const long at = (long)kv_head * DH + 8 * (lq & 3);
-    put_columns<DB>(dk[nb], bias.scale, dK.p + (long)b * dK.batch + k * dK.row + at, k < Lk, lane);
-    put_columns<DB>(dv[nb], 1.0f, dV.p + (long)b * dV.batch + k * dV.row + at, k < Lk, lane);
+    put_columns<DB>(dk[nb], bias.scale, dK.p + (long)b * dK.batch + k * dK.row + at, k < (int)Lk, lane);
+    put_columns<DB>(dv[nb], 1.0f, dV.p + (long)b * dV.batch + k * dV.row + at, k < (int)Lk, lane);
   }
 #endif
 }
