@@ -48,7 +48,8 @@ __device__ __forceinline__ float row_exponent(float lse, bool live) {
 // lane with a query's logits and their gradients as the operand of dQ^T += K^T dS^T. Fragments are read some slots before the MFMAs that use them, in
 // the order written: left to itself the compiler reads them as they are needed, and a wave waits for the LDS at every one.
 // Two waves on a SIMD take turns with the vector and the matrix pipe. With 32 queries a wave half the LDS reads would do, but one wave a SIMD is all that
-// the registers hold then (heads of 128, 8191 tokens: first pass 788 us, second 1104; so 610 and 860).
+// the registers hold then (heads of 128, 8191 tokens: first pass 788 us, second 1104; so 610 and 860). First pass in workgroups of four waves, two to a unit: 720;
+// with four of the eight waves a phase behind the others, so that the pipes have different work: 800.
 // ---------------------------------------------------------------------------
 constexpr int kWaves = 8;
 
@@ -687,8 +688,9 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
     hipLaunchKernelGGL((bias_dq_kernel<DH>), dim3((unsigned)((long)a->B * a->H * at.nq)), dim3(64 * kWaves), lds_q, s, q, k, v, o, rest, d, gq, lse,  \
                        delta, bias, (long)a->Lq, (long)a->Lk, a->B, a->H, a->H / a->Hk, at.nq);                                               \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
-    hipLaunchKernelGGL((bias_dkv_kernel<DH>), dim3((unsigned)((long)a->B * a->Hk * at.nk)), dim3(KeyShape<DH>::kThreads), KeyShape<DH>::lds(bias.width()), s, q, k, v, d, gk, gv, lse,     \
-                       delta, part, bias, (long)a->Lq, (long)a->Lk, a->B, a->H, a->H / a->Hk, at.nk);                                                     \
+    hipLaunchKernelGGL((bias_dkv_kernel<DH>), dim3((unsigned)((long)a->B * a->Hk * at.nk)), dim3(KeyShape<DH>::kThreads),                             \
+                       KeyShape<DH>::lds(bias.width()), s, q, k, v, d, gk, gv, lse, delta, part, bias, (long)a->Lq, (long)a->Lk, a->B, a->H,          \
+                       a->H / a->Hk, at.nk);                                                                                                          \
     CHORUS_LAUNCH_CHECK();                                                                                                                    \
   } while (0)
   if (a->dh == 128) BACKWARD(128);
