@@ -626,6 +626,38 @@ __global__ __launch_bounds__(256) void bias_dtable_kernel(const double* __restri
   if (lane == 0) dtable[(long)c * H + head] = (float)a;
 }
 
+// Both in one launch, a workgroup a head, where sequences times tiles of keys are few: a pass with both directions, which the host's side bounds then, takes 44.9
+// us with one tile of keys and 48.0 with two launches, 46.4 and 48.5 with 8, 148.3 and 149.6 with 16 of 64 heads; 90.6 and 89.9 with 32, 1176 and 1125 with 1024.
+constexpr long kFewParts = 16;
+constexpr int kTableThreads = 1024;
+__global__ __launch_bounds__(kTableThreads) void bias_table_kernel(const float* __restrict__ part, float* __restrict__ dtable, BiasArgs bias, int B, int H,
+                                                                   int nk) {
+  constexpr int HALF = kTableThreads / 2, MOST = 2 * (kMostFar + kPad) + 1;
+  __shared__ double s_sum[2][MOST];
+  __shared__ int s_bucket[MOST];
+  const int tid = threadIdx.x, head = blockIdx.x, width = bias.width(), n = B * nk, share = tid / HALF;
+  for (int i = tid; i < width; i += kTableThreads) s_bucket[i] = bias.bucket_of(i);
+  for (int i = tid % HALF; i < width; i += HALF) {
+    double a = 0.0;
+#pragma unroll 8
+    for (int k = share; k < n; k += 2) {
+      const int b = k / nk;
+      a += (double)part[(((long)b * H + head) * nk + (k - b * nk)) * width + i];
+    }
+    s_sum[share][i] = a;
+  }
+  __syncthreads();
+  const int lane = tid & 63;
+  for (int c = tid >> 6; c < bias.n_buckets; c += kTableThreads / 64) {
+    double a = 0.0;
+    for (int i = lane; i < width; i += 64)
+      if (s_bucket[i] == c) a += s_sum[0][i] + s_sum[1][i];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) a += __shfl_xor(a, d);
+    if (lane == 0) dtable[(long)c * H + head] = (float)a;
+  }
+}
+
 struct BackwardLayout {
   size_t delta, apart, part, sums, all;
   int nq, nk;
@@ -696,6 +728,11 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
   if (a->dh == 128) BACKWARD(128);
   else BACKWARD(64);
 #undef BACKWARD
+  if ((long)a->B * at.nk <= kFewParts) {
+    hipLaunchKernelGGL(bias_table_kernel, dim3((unsigned)a->H), dim3(kTableThreads), 0, s, (const float*)part, dtable, bias, a->B, a->H, at.nk);
+    CHORUS_LAUNCH_CHECK();
+    return CHORUS_OK;
+  }
   double* const sums = reinterpret_cast<double*>(static_cast<uint8_t*>(ws) + at.sums);
   hipLaunchKernelGGL(bias_distances_kernel, dim3((unsigned)((bias.width() + 63) / 64), (unsigned)a->H), dim3(256), 0, s, (const float*)part, sums,
                      bias.width(), a->B, a->H, at.nk);

@@ -8,7 +8,7 @@ from test_kernel_resources import _scratch
 @pytest.mark.parametrize("source,count,full,most", [
     ("gemm_i8.hip", 28, (), 0), ("gated.hip", 26, ("gated_kernelILi0ELb1ELi8ELi8", "gated_kernelILi1ELb1ELi8ELi8"), 12),
     ("bias_attention.hip", 10, ("bias_few_kernelILi128E", "bias_attention_kernelILi64ELb1E"), 16),
-    ("bias_attention_backward.hip", 6, ("bias_dkv_kernelILi64E",), 20),
+    ("bias_attention_backward.hip", 7, ("bias_dkv_kernelILi64E",), 20),
 ])
 def test_scratch(source, count, full, most, tmp_path):
     got = _scratch(source, tmp_path)
