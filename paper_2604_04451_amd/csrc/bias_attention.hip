@@ -463,7 +463,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = 0.f, l_run = 0.f;  // reference, in powers of two, and this lane's share of the sum of the weights
-  bool seen = false;
+  bool holds = false;              // something is left of that sum
   for (; t < t1; t += kFewWaves) {
     f32x4 s[KB];
 #pragma unroll
@@ -499,9 +499,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
         for (int i = 0; i < 4; ++i)
           if (16 * kb + i >= left) here[kb][i] = -INFINITY;
     }
-    // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a reference that has gone far up is
-    // looked at once more.
+    // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a reference that has gone far up, from a mask's
+    // size to that of the keys behind it, is looked at once more: it is off by a rounding of the mask then. As it has left nothing of the sums, it may go down.
     const auto exponent = [&](int kb, int i, float by) { return __builtin_fmaf(s[kb][i], by, here[kb][i] - m_run); };
+    bool finite = false;
 #pragma unroll 1
     for (int again = 0; again < 2; ++again) {
       const float by = products_by(scale, m_run);
@@ -510,18 +511,19 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, exponent(kb, i, by));
-      if (!__any(!seen || mx > 8.0f)) break;  // as in the tiled kernel
+      if (!__any(!holds || mx > 8.0f)) break;  // as in the tiled kernel
       float m = fmaxf(mx, swap_rows16(mx));
       m = fmaxf(m, swap_halves(m));
-      const bool finite = m > -INFINITY;
-      const float up = !seen ? (finite ? m : 0.f) : fmaxf(m, 0.f);
-      const float alpha = !seen ? 1.0f : __builtin_amdgcn_exp2f(-up);
-      seen = seen || finite;
+      finite = m > -INFINITY;
+      const float up = holds ? fmaxf(m, 0.f) : finite ? m : 0.f;
+      const float alpha = holds ? __builtin_amdgcn_exp2f(-up) : 1.0f;
+      holds = holds && alpha > 0.f;
       m_run += up;
       l_run *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
     }
+    holds = holds || finite;
     const float by = products_by(scale, m_run);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
