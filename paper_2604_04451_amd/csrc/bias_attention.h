@@ -13,8 +13,8 @@ constexpr int64_t kMostTokens = 1 << 28;
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A row's reference, or the exponent of its sum, goes into the sums of the matrix pipe, whose roundings are of its size then: 2^-14 each at this limit, in
 // powers of two. Rows beyond it, which a large finite bias is all that is left to (or a large positive one), have no weights in the loops; a wave makes them
-// by itself behind those, in fp32, taking the reference off the bias before the product is added. No reference is below kLeastReference: a row that has
-// seen only keys with a bias of -10000, or of the lowest value of the type, has lost nothing when it sees others.
+// by itself behind those, in fp32, taking the reference off the bias before the product is added, by a reference in two parts (Reference). No reference in the
+// loops is below kLeastReference: a row that has seen only keys with a bias of -10000, or of the lowest value of the type, has lost nothing when it sees others.
 constexpr float kMostInSums = 1024.f, kLeastReference = -32.f, kLeastSum = 0x1p-90f;
 // What multiplies the products of a row: nothing is left of them beside a reference of a size that leaves nothing of them in 64 bits either. A row that has
 // nothing but biases of the lowest value of the type has all its keys alike.
@@ -22,6 +22,23 @@ __device__ __forceinline__ float products_by(float scale, float reference) { ret
 __device__ __forceinline__ bool out_of_sums(float exponent) {
   return __builtin_fabsf(exponent) > kMostInSums && __builtin_fabsf(exponent) < INFINITY;
 }
+
+// What is taken off the logits of a row, in two parts: beside a bias of -1e10 one number in fp32 has no room for a product of 100. hi is near the largest
+// bias, so that bias - hi is exact where it matters, and lo what is left of the largest logit.
+struct Reference {
+  float hi, lo;
+  // up by so much; what the sum's rounding leaves off goes to lo
+  __device__ __forceinline__ void move(float up) {
+    const float t = lo + up, to = hi + t, moved = to - hi;
+    lo = (hi - (to - moved)) + (t - moved);
+    hi = to;
+  }
+};
+// A share of a row: its reference and the sum of its weights, 0 where it has no key.
+struct Share {
+  Reference ref;
+  float sum;
+};
 
 // A tensor of heads as the kernels see it: value (b, row, head, i) at p + b * batch + row * row_step + head * dh + i.
 struct Rows {
@@ -222,16 +239,26 @@ struct ApartRow {
     }
     return sum;
   }
-  // logit of key j less ref
-  __device__ __forceinline__ float logit(int j, float ref) const {
+  Reference ref;          // of its keys, once refer() has found it
+
+  __device__ __forceinline__ int place(int j) const {  // of key j's bias
     const int at = nearest + j + far + kPad, last = 2 * (far + kPad);
-    return __builtin_fmaf(product(q, k + (long)j * k_row), products_by(scale, ref), s_bias[at < 0 ? 0 : at < last ? at : last] - ref);
+    return at < 0 ? 0 : at < last ? at : last;
   }
-  __device__ __forceinline__ float most(int j0, int j1, int lane) const {
+  // logit of key j less the reference
+  __device__ __forceinline__ float logit(int j) const {
+    return __builtin_fmaf(product(q, k + (long)j * k_row), products_by(scale, ref.hi), (s_bias[place(j)] - ref.hi) - ref.lo);
+  }
+  __device__ __forceinline__ void refer(int j0, int j1, int lane) {
     float m = -INFINITY;
+    for (int i = place(j0) + lane, last = place(j1 - 1); i <= last; i += 64) m = fmaxf(m, s_bias[i]);
+    m = wave_max(m);
+    ref = Reference{m > -INFINITY ? m : 0.f, 0.f};
+    m = -INFINITY;
 #pragma unroll 1
-    for (int j = j0 + lane; j < j1; j += 64) m = fmaxf(m, logit(j, 0.f));
-    return wave_max(m);
+    for (int j = j0 + lane; j < j1; j += 64) m = fmaxf(m, logit(j));
+    m = wave_max(m);
+    ref.lo = m > -INFINITY ? m : 0.f;
   }
   // sum[e] = the sum over keys j0 .. j1 of weight(j) rows[j][lane + 64 e]; weight(j) is asked of lane j - j0 - 64 i
   template <class WEIGHT>

@@ -28,7 +28,7 @@ int slices_of(long tiles, long Lk) {
   return s < 1 ? 1 : s > kMostSlices ? kMostSlices : (int)s;
 }
 size_t slice_bytes(long tiles, int slices, int dh, int rows) {
-  return slices > 1 ? (size_t)tiles * slices * rows * (dh * sizeof(float) + sizeof(float2)) : 0;
+  return slices > 1 ? (size_t)tiles * slices * rows * (dh * sizeof(float) + sizeof(Share)) : 0;
 }
 
 struct Outputs {
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
         if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
       }
       if (g == 0 && mine_live)
-        reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - qb * kTileQueries)] = make_float2(m_run[rb], l);
+        reinterpret_cast<Share*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - qb * kTileQueries)] = Share{{m_run[rb], 0.f}, l};
       continue;
     }
     const long to = (long)b * out.o.batch + row * out.o.row + (long)head * DH + 8 * b4;
@@ -352,11 +352,11 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     for (uint32_t left = all_apart; left; left &= left - 1) {
       const int r = wave * 32 + __builtin_ctz(left), q = qb2 * kTileQueries + r, see = !bias.causal || origin + q + 1 > n ? n : origin + q + 1;
       const int j0 = t0 * kTileKeys, j1 = t1 * kTileKeys < see ? t1 * kTileKeys : see;
-      const ApartRow<DH> x{Q.p + (long)b2 * Q.batch + q * Q.row + (long)head2 * DH, keys, K.row, s_bias, -(origin + q), far, scale};
-      const float m = x.most(j0, j1, at2);
+      ApartRow<DH> x{Q.p + (long)b2 * Q.batch + q * Q.row + (long)head2 * DH, keys, K.row, s_bias, -(origin + q), far, scale, {0.f, 0.f}};
+      x.refer(j0, j1, at2);
       float sum[DH / 64], total = 0.f;
       ApartRow<DH>::weighted([&](int j) {
-        const float w = __builtin_amdgcn_exp2f(x.logit(j, m));
+        const float w = __builtin_amdgcn_exp2f(x.logit(j));
         total += w;
         return w;
       }, values, V.row, j0, j1, at2, sum);
@@ -374,8 +374,8 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
         }
       }
       if (at2 == 0) {
-        if (slices > 1) reinterpret_cast<float2*>(part + (long)gridDim.x * kTileQueries * DH)[row] = make_float2(m, total);
-        else if (out.lse) out.lse[((long)b2 * H + head2) * Lq + q] = kLn2 * (m + __builtin_amdgcn_logf(total));
+        if (slices > 1) reinterpret_cast<Share*>(part + (long)gridDim.x * kTileQueries * DH)[row] = Share{x.ref, total};
+        else if (out.lse) out.lse[((long)b2 * H + head2) * Lq + q] = kLn2 * (x.ref.hi + (x.ref.lo + __builtin_amdgcn_logf(total)));
       }
     }
   }
@@ -462,8 +462,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   f32x4 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = 0.f, l_run = 0.f;  // reference, in powers of two, and this lane's share of the sum of the weights
-  bool holds = false;              // something is left of that sum
+  Reference ref{0.f, 0.f};  // in powers of two
+  float l_run = 0.f;        // this lane's share of the sum of the weights
+  bool holds = false;       // something is left of that sum
   for (; t < t1; t += kFewWaves) {
     f32x4 s[KB];
 #pragma unroll
@@ -499,13 +500,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
         for (int i = 0; i < 4; ++i)
           if (16 * kb + i >= left) here[kb][i] = -INFINITY;
     }
-    // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a reference that has gone far up, from a mask's
-    // size to that of the keys behind it, is looked at once more: it is off by a rounding of the mask then. As it has left nothing of the sums, it may go down.
-    const auto exponent = [&](int kb, int i, float by) { return __builtin_fmaf(s[kb][i], by, here[kb][i] - m_run); };
+    // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a row's first reference, and one that has gone
+    // far up, from a mask's size to that of the keys behind it, is looked at once more: the largest logit was off by a rounding of the mask then. As there is
+    // nothing in the sums, it may go down.
+    const auto exponent = [&](int kb, int i, float by) { return __builtin_fmaf(s[kb][i], by, (here[kb][i] - ref.hi) - ref.lo); };
     bool finite = false;
 #pragma unroll 1
     for (int again = 0; again < 2; ++again) {
-      const float by = products_by(scale, m_run);
+      const float by = products_by(scale, ref.hi);
       float mx = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -518,13 +520,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       const float up = holds ? fmaxf(m, 0.f) : finite ? m : 0.f;
       const float alpha = holds ? __builtin_amdgcn_exp2f(-up) : 1.0f;
       holds = holds && alpha > 0.f;
-      m_run += up;
+      ref.move(up);
       l_run *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
     }
     holds = holds || finite;
-    const float by = products_by(scale, m_run);
+    const float by = products_by(scale, ref.hi);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -546,28 +548,34 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   l_run += swap_rows16(l_run);
   l_run += swap_halves(l_run);
 
-  // the waves' results, [wave][row][DH] and (reference, sum): put together in the order of the waves
+  // the waves' results, [wave][row][DH] and their shares: put together in the order of the waves
   lds_barrier();
   float* const s_o = reinterpret_cast<float*>(smem);
-  float2* const s_ml = reinterpret_cast<float2*>(s_o + kFewWaves * kFewRows * (DH + 4));
+  Share* const s_share = reinterpret_cast<Share*>(s_o + kFewWaves * kFewRows * (DH + 4));
 #pragma unroll
   for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(s_o + (wave * kFewRows + lq) * (DH + 4) + 16 * db + 4 * g) = o[db];
-  if (g == 0) s_ml[wave * kFewRows + lq] = make_float2(m_run, l_run);
+  if (g == 0) s_share[wave * kFewRows + lq] = Share{ref, l_run};
   lds_barrier();
   constexpr int PER = 64 * kFewWaves / kFewRows, E = DH / PER;  // threads of a row; values of a thread
   const int r = tid / PER, d0 = tid % PER * E;
   if (r >= live_rows) return;
-  float top = -INFINITY, total = 0.f, sum[E] = {};
+  Reference top{-INFINITY, -INFINITY};
+  float total = 0.f, sum[E] = {};
 #pragma unroll
   for (int w = 0; w < kFewWaves; ++w) {
-    const float2 ml = s_ml[w * kFewRows + r];
-    if (ml.y != 0.f) top = fmaxf(top, ml.x);
+    const Share x = s_share[w * kFewRows + r];
+    if (x.sum != 0.f) top.hi = fmaxf(top.hi, x.ref.hi);
   }
 #pragma unroll
   for (int w = 0; w < kFewWaves; ++w) {
-    const float2 ml = s_ml[w * kFewRows + r];
-    const float f = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-    total = __builtin_fmaf(f, ml.y, total);
+    const Share x = s_share[w * kFewRows + r];
+    if (x.sum != 0.f) top.lo = fmaxf(top.lo, (x.ref.hi - top.hi) + x.ref.lo);
+  }
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) {
+    const Share x = s_share[w * kFewRows + r];
+    const float f = x.sum != 0.f ? __builtin_amdgcn_exp2f((x.ref.hi - top.hi) + x.ref.lo - top.lo) : 0.f;
+    total = __builtin_fmaf(f, x.sum, total);
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] = __builtin_fmaf(f, s_o[(w * kFewRows + r) * (DH + 4) + d0 + e], sum[e]);
   }
@@ -575,7 +583,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
     float* op = part + ((long)unit * kFewRows + r) * DH + d0;
 #pragma unroll
     for (int e = 0; e < E; ++e) op[e] = sum[e];
-    if (d0 == 0) reinterpret_cast<float2*>(part + (long)gridDim.x * kFewRows * DH)[(long)unit * kFewRows + r] = make_float2(total == 0.f ? 0.f : top, total);
+    if (d0 == 0) reinterpret_cast<Share*>(part + (long)gridDim.x * kFewRows * DH)[(long)unit * kFewRows + r] = Share{top, total};
     return;
   }
   const int head = head0 + r / Lq, qi = r % Lq;
@@ -583,7 +591,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   uint16_t* op = out.o.p + (long)b * out.o.batch + (long)qi * out.o.row + (long)head * DH + d0;
 #pragma unroll
   for (int e = 0; e < E; ++e) op[e] = f32_to_bf16(sum[e] * inv);
-  if (out.lse && d0 == 0) out.lse[((long)b * H + head) * Lq + qi] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+  if (out.lse && d0 == 0) out.lse[((long)b * H + head) * Lq + qi] = total == 0.f ? -INFINITY : kLn2 * (top.hi + (top.lo + __builtin_amdgcn_logf(total)));
 #endif
 }
 
@@ -616,10 +624,12 @@ __global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict_
     if (q >= Lq) return;
   }
   const long first = tile * slices * ROWS + row;
-  const float2 ml = lane < slices ? reinterpret_cast<const float2*>(part + units * ROWS * DH)[first + (long)lane * ROWS] : make_float2(0.f, 0.f);
-  const float top = wave_max(ml.y != 0.f ? ml.x : -INFINITY);  // a slice without a key has no reference
-  const float w = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-  const float total = wave_sum(w * ml.y), inv = total == 0.f ? 0.f : 1.0f / total;
+  Share x{{0.f, 0.f}, 0.f};
+  if (lane < slices) x = reinterpret_cast<const Share*>(part + units * ROWS * DH)[first + (long)lane * ROWS];
+  const bool some = x.sum != 0.f;  // a slice without a key has no reference
+  const float hi = wave_max(some ? x.ref.hi : -INFINITY), behind = (x.ref.hi - hi) + x.ref.lo, lo = wave_max(some ? behind : -INFINITY);
+  const float w = some ? __builtin_amdgcn_exp2f(behind - lo) : 0.f;
+  const float total = wave_sum(w * x.sum), inv = total == 0.f ? 0.f : 1.0f / total;
   float sum[E] = {};
   for (int s = 0; s < slices; ++s) {
     const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
@@ -634,7 +644,7 @@ __global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict_
     out.o.p[to + e] = f32_to_bf16(v);
     if (out.rest) out.rest[to + e] = left_off(v);
   }
-  if (out.lse && lane == 0) out.lse[((long)b * H + head) * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+  if (out.lse && lane == 0) out.lse[((long)b * H + head) * Lq + q] = total == 0.f ? -INFINITY : kLn2 * (hi + (lo + __builtin_amdgcn_logf(total)));
 }
 
 struct ForwardPlan {

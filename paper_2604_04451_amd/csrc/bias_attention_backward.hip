@@ -11,8 +11,8 @@
 namespace chorus {
 namespace {
 
-// What the first pass leaves the second of every row: delta, and where it is out of the sums also its reference and the logarithm of its sum by that; and
-// which rows those are, a bit a row, 16 rows a word.
+// What the first pass leaves the second of every row: delta, and where it is out of the sums also its reference's first part, and the second with the logarithm
+// of its sum; and which rows those are, a bit a row, 16 rows a word.
 struct Delta {
   float* p;  // [3][B, H, Lq]
   long step;  // B * H * Lq
@@ -228,22 +228,22 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     for (uint32_t left = apart; left; left &= left - 1) {
       const int r = q0 + __builtin_ctz(left), see = !bias.causal || origin + r + 1 > n ? n : origin + r + 1;
       const uint16_t* const dp = dO.p + (long)b * dO.batch + r * dO.row + (long)head * DH;
-      const ApartRow<DH> x{Q.p + (long)b * Q.batch + r * Q.row + (long)head * DH, k_base, K.row, s_bias, -(origin + r), far, scale};
-      const float m = x.most(0, see, lane);
+      ApartRow<DH> x{Q.p + (long)b * Q.batch + r * Q.row + (long)head * DH, k_base, K.row, s_bias, -(origin + r), far, scale, {0.f, 0.f}};
+      x.refer(0, see, lane);
       float l = 0.f, d = 0.f, sum[DH / 64];
 #pragma unroll 1
       for (int j = lane; j < see; j += 64) {
-        const float w = __builtin_amdgcn_exp2f(x.logit(j, m));
+        const float w = __builtin_amdgcn_exp2f(x.logit(j));
         l += w;
         d = __builtin_fmaf(w, x.product(dp, v_base + (long)j * V.row), d);
       }
       l = wave_sum(l);
       d = wave_sum(d) / l;
-      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j, m)) / l * (x.product(dp, v_base + (long)j * V.row) - d); }, k_base, K.row, 0, see,
+      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j)) / l * (x.product(dp, v_base + (long)j * V.row) - d); }, k_base, K.row, 0, see,
                              lane, sum);
 #pragma unroll
       for (int e = 0; e < DH / 64; ++e) dQ.p[(long)b * dQ.batch + r * dQ.row + (long)head * DH + lane + 64 * e] = f32_to_bf16(sum[e] * bias.scale);
-      if (lane < 3) delta.p[lane * delta.step + bh * Lq + r] = lane == 0 ? d : lane == 1 ? m : __builtin_amdgcn_logf(l);
+      if (lane < 3) delta.p[lane * delta.step + bh * Lq + r] = lane == 0 ? d : lane == 1 ? x.ref.hi : x.ref.lo + __builtin_amdgcn_logf(l);
     }
   }
   put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3),
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
             const int dist = k0 + 16 * nb + lq - (origin + r), at = dist + far + kPad;
             const bool sees = counts[nb] && !(bias.causal && dist > 0);
             const float bias_here = s_bias[at < 0 ? 0 : at < width ? at : width - 1];
-            const float pw = sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(x, products_by(scale, ref), bias_here - ref) - log_sum) : 0.f;
+            const float pw = sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(x, products_by(scale, ref), (bias_here - ref) - log_sum)) : 0.f;
             const float dsw = sees ? pw * (y - dl) : 0.f;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
