@@ -67,6 +67,11 @@ struct BiasArgs {
     const int f = first ? first[b] : 0;
     return f < -most ? -most : f > most ? most : f;
   }
+  // keys that a query at position `last` or ahead of it sees: those behind are as if they were not there
+  __device__ __forceinline__ int seen(int b, long Lk, int last) const {
+    const int n = keys(b, Lk);
+    return !causal || last + 1 > n ? n : last < 0 ? 0 : last + 1;
+  }
   __host__ __device__ int width() const { return 2 * (far + kPad) + 1; }  // distances that a bias or a sum is kept for, the ends repeated
   // bucket of distance i - (far + kPad)
   __device__ __forceinline__ int bucket_of(int i) const {
@@ -219,7 +224,7 @@ struct ColumnFragments {
   }
 };
 
-// A row that is out of the sums, made by a wave: a key a lane for the logits, a value of the result (of each 64) a lane for what is weighted by them.
+// A row by itself, made by a wave of the keys that it sees: a key a lane for the logits, a value of the result (of each 64) a lane for what is weighted by them.
 template <int DH>
 struct ApartRow {
   const uint16_t* q;      // the row
@@ -279,6 +284,12 @@ struct ApartRow {
     }
   }
 };
+
+// Rows l % 16 of which some lane l has the bit
+__device__ __forceinline__ uint32_t rows_of_lanes(uint64_t lanes) {
+  lanes |= lanes >> 32;
+  return (uint32_t)(lanes | lanes >> 16) & 0xffff;
+}
 
 __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

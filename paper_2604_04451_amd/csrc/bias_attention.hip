@@ -53,15 +53,11 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
   const int lq = lane & 15, g = lane >> 4;
   const Place place = place_of(blockIdx.x, gridDim.x, B, H, nq, slices);
   const int b = place.b, head = place.head, qb = place.tile, slice = place.slice, unit = ((head * B + b) * nq + qb) * slices + slice;
-  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int q0 = qb * kTileQueries + wave * 32;  // the wave's first query
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
-  int most = n;  // keys that some query of the workgroup sees
-  if (bias.causal) {
-    const int m = origin + last_q + 1;
-    most = m < 0 ? 0 : m < n ? m : n;
-  }
-  const int steps = (most + kTileKeys - 1) / kTileKeys;
+  const int n = __builtin_amdgcn_readfirstlane(bias.seen(b, Lk, origin + last_q));  // keys that some query of the workgroup sees
+  const int steps = (n + kTileKeys - 1) / kTileKeys;
   const int t0 = slices > 1 ? steps * slice / slices : 0, t1 = slices > 1 ? steps * (slice + 1) / slices : steps;  // at most 2^22 steps and 64 slices
 
   BiasFill<256> fill;
@@ -294,7 +290,9 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 
   // On the way out four neighbouring lanes write 64 bytes of a row: they get them from the lanes of that row.
   const auto from_lane = [](int src, uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * src, (int)v); };
-  const int row0 = q0 + (lq & 12) + g, b4 = lq & 3;
+  int out_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(out_lane));  // the lane again: what is made of it would take registers that the loop needs
+  const int out_q = out_lane & 15, out_g = out_lane >> 4, row0 = q0 + (out_q & 12) + out_g, b4 = out_q & 3;
   uint32_t all_apart = 0;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -303,11 +301,17 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       l_run[rb] += swap_halves(l_run[rb]);
     }
     const float l = SPLIT ? l_run[rb] : l_sum[rb][0], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
-    const int row = row0 + 16 * rb, mine = q0 + 16 * rb + lq, count = (int)Lq;
-    // rows that are out of the sums: all their logits are far below the reference, or it is too large
-    const uint32_t apart = (uint32_t)__ballot(mine < count && seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))) & 0xffff;
+    const int row = row0 + 16 * rb, mine = q0 + 16 * rb + out_q, count = (int)Lq;
+    // rows that are out of the sums: all their logits are far below the reference, or it is too large. And rows that are not finite, which may be so by
+    // an infinity or NaN times the weight 0 of a key that they do not see, or the other part of a weight.
+    float none = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) none = __builtin_fmaf(o[db][rb][i], 0.f, none);
+    const uint32_t apart = rows_of_lanes(__ballot(mine < count && (!(none == 0.f) || (seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))))));
     all_apart |= apart << 16 * rb;
-    const bool live = row < count && !(apart >> ((lq & 12) + g) & 1), mine_live = mine < count && !(apart >> lq & 1);
+    const bool live = row < count && !(apart >> ((out_q & 12) + out_g) & 1), mine_live = mine < count && !(apart >> out_q & 1);
     if (slices > 1) {
       const long at = (long)unit * kTileQueries;
       float* op = part + (at + (row - qb * kTileQueries)) * DH + 4 * b4;
@@ -315,15 +319,15 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       for (int db = 0; db < DB; ++db) {
         f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(from_lane(16 * b4 + (lq & 12) + g, __float_as_uint(o[db][rb][e])));
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(from_lane(16 * b4 + (out_q & 12) + out_g, __float_as_uint(o[db][rb][e])));
         if (live) *reinterpret_cast<f32x4*>(op + 16 * db) = v;
       }
-      if (g == 0 && mine_live)
+      if (out_g == 0 && mine_live)
         reinterpret_cast<Share*>(part + (long)gridDim.x * kTileQueries * DH)[at + (mine - qb * kTileQueries)] = Share{{m_run[rb], 0.f}, l};
       continue;
     }
     const long to = (long)b * out.o.batch + row * out.o.row + (long)head * DH + 8 * b4;
-    const int src = 16 * (b4 >> 1 | (b4 & 1) << 1) + (lq & 12) + g;
+    const int src = 16 * (b4 >> 1 | (b4 & 1) << 1) + (out_q & 12) + out_g;
     auto put = [&](uint16_t* p, bool rest) {
 #pragma unroll
       for (int i = 0; i < DB / 2; ++i) {
@@ -341,11 +345,11 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     };
     put(out.o.p, false);
     if (SPLIT) put(out.rest, true);
-    if (out.lse && g == 0 && mine_live) out.lse[((long)b * H + head) * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
+    if (out.lse && out_g == 0 && mine_live) out.lse[((long)b * H + head) * Lq + mine] = l == 0.f ? -INFINITY : kLn2 * (m_run[rb] + __builtin_amdgcn_logf(l));
   }
   if (__builtin_expect(all_apart != 0, 0)) {
     // places worked out again: kept from the start they would take registers that the loop needs
-    int b2 = __builtin_amdgcn_readfirstlane(b), head2 = __builtin_amdgcn_readfirstlane(head), qb2 = __builtin_amdgcn_readfirstlane(qb), at2 = threadIdx.x & 63;
+    int b2 = __builtin_amdgcn_readfirstlane(b), head2 = __builtin_amdgcn_readfirstlane(head), qb2 = __builtin_amdgcn_readfirstlane(qb), at2 = out_lane;
     asm volatile("" : "+s"(b2), "+s"(head2), "+s"(qb2), "+v"(at2));
     const uint16_t* const keys = K.p + (long)b2 * K.batch + (long)(head2 / group) * DH;
     const uint16_t* const values = V.p + (long)b2 * V.batch + (long)(head2 / group) * DH;
@@ -361,13 +365,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
         return w;
       }, values, V.row, j0, j1, at2, sum);
       total = wave_sum(total);
+      const bool some = total != 0.f;
       const long row = (long)(((head2 * B + b2) * nq + qb2) * slices + slice) * kTileQueries + r;
 #pragma unroll
       for (int e = 0; e < DH / 64; ++e) {
         if (slices > 1) {
-          part[row * DH + at2 + 64 * e] = sum[e];
+          part[row * DH + at2 + 64 * e] = some ? sum[e] : 0.f;
         } else {
-          const float v = sum[e] / total;
+          const float v = some ? sum[e] / total : 0.f;
           const long to = (long)b2 * out.o.batch + q * out.o.row + (long)head2 * DH + at2 + 64 * e;
           out.o.p[to] = f32_to_bf16(v);
           if (SPLIT) out.rest[to] = left_off(v);
@@ -375,7 +380,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
       }
       if (at2 == 0) {
         if (slices > 1) reinterpret_cast<Share*>(part + (long)gridDim.x * kTileQueries * DH)[row] = Share{x.ref, total};
-        else if (out.lse) out.lse[((long)b2 * H + head2) * Lq + q] = kLn2 * (x.ref.hi + (x.ref.lo + __builtin_amdgcn_logf(total)));
+        else if (out.lse) out.lse[((long)b2 * H + head2) * Lq + q] = some ? kLn2 * (x.ref.hi + (x.ref.lo + __builtin_amdgcn_logf(total))) : -INFINITY;
       }
     }
   }
@@ -409,13 +414,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
   const int in_group = tile % place.parts, bk = tile / place.parts, b = bk / Hk, kv_head = bk - b * Hk;
   const int head0 = kv_head * group + in_group * place.heads;
   const int heads = group - in_group * place.heads < place.heads ? group - in_group * place.heads : place.heads;
-  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int origin = __builtin_amdgcn_readfirstlane(bias.origin(b)), n = __builtin_amdgcn_readfirstlane(bias.seen(b, Lk, origin + Lq - 1));
   const int live_rows = heads * Lq, row = lq < live_rows ? lq : live_rows - 1, of_head = row / Lq, q = row - of_head * Lq;
-  int most = n;  // keys that some query sees
-  if (bias.causal) most = origin + Lq < 0 ? 0 : origin + Lq < n ? origin + Lq : n;
-  const int steps = (most + kTileKeys - 1) / kTileKeys;
-  const int t1 = slices > 1 ? steps * (slice + 1) / slices : steps;
-  int t = (slices > 1 ? steps * slice / slices : 0) + wave;
+  const int steps = (n + kTileKeys - 1) / kTileKeys;
+  const int t0 = (slices > 1 ? steps * slice / slices : 0) + wave, t1 = slices > 1 ? steps * (slice + 1) / slices : steps;
+  int t = t0;
 
   BiasFill<64 * kFewWaves> fill;
   fill.buckets(bias, tid);
@@ -498,7 +501,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (16 * kb + i >= left) here[kb][i] = -INFINITY;
+          if (16 * kb + i >= left) {
+            here[kb][i] = -INFINITY;
+            s[kb][i] = 0.f;
+          }
     }
     // Bias less reference first: both can be of a size that leaves nothing of the products. For the same reason a row's first reference, and one that has gone
     // far up, from a mask's size to that of the keys behind it, is looked at once more: the largest logit was off by a rounding of the mask then. As there is
@@ -555,6 +561,27 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
 #pragma unroll
   for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(s_o + (wave * kFewRows + lq) * (DH + 4) + 16 * db + 4 * g) = o[db];
   if (g == 0) s_share[wave * kFewRows + lq] = Share{ref, l_run};
+  // Rows that are not finite are made again of the keys that they see, as in the tiled kernel: this wave's part of them, with its weights.
+  float none = 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) none = __builtin_fmaf(o[db][i], 0.f, none);
+  for (uint32_t left = rows_of_lanes(__ballot(lq < live_rows && !(none == 0.f))); __builtin_expect(left != 0, 0); left &= left - 1) {
+    const int r = __builtin_ctz(left), of = r / Lq, qi = r - of * Lq, see = !bias.causal || origin + qi + 1 > n ? n : origin + qi + 1;
+    const Reference at{__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ref.hi), r)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ref.lo), r))};
+    const ApartRow<DH> x{Q.p + (long)b * Q.batch + (long)qi * Q.row + (long)(head0 + of) * DH, k_base, K.row, s_bias + of * width, -(origin + qi), far, scale, at};
+    float sum[DH / 64] = {};
+    for (int i = t0; i < t1; i += kFewWaves) {
+      const int j0 = i * kTileKeys, j1 = j0 + kTileKeys < see ? j0 + kTileKeys : see;
+      float here[DH / 64];
+      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j)); }, v_base, V.row, j0, j1, lane, here);
+#pragma unroll
+      for (int e = 0; e < DH / 64; ++e) sum[e] += here[e];
+    }
+#pragma unroll
+    for (int e = 0; e < DH / 64; ++e) s_o[(wave * kFewRows + r) * (DH + 4) + lane + 64 * e] = sum[e];
+  }
   lds_barrier();
   constexpr int PER = 64 * kFewWaves / kFewRows, E = DH / PER;  // threads of a row; values of a thread
   const int r = tid / PER, d0 = tid % PER * E;
