@@ -69,15 +69,11 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   const Place place = place_of(blockIdx.x, gridDim.x, B, H, nq, 1);
   const int b = place.b, head = place.head, qb = place.tile;
   const long bh = (long)b * H + head;
-  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
   const int q0 = qb * kTileQueries + wave * 16;
   const int last_q = (int)((long)(qb + 1) * kTileQueries < Lq ? (qb + 1) * kTileQueries : Lq) - 1;
-  int most = n;
-  if (bias.causal) {
-    const int m = origin + last_q + 1;
-    most = m < 0 ? 0 : m < n ? m : n;
-  }
-  const int steps = (most + kTileKeys - 1) / kTileKeys;
+  const int n = __builtin_amdgcn_readfirstlane(bias.seen(b, Lk, origin + last_q));  // keys that some query of the workgroup sees
+  const int steps = (n + kTileKeys - 1) / kTileKeys;
 
   TileStage<DH, THREADS> k_in(tid, K.row), v_in(tid, V.row);
   const uint16_t* const k_base = K.p + (long)b * K.batch + (long)(head / group) * DH;
@@ -221,11 +217,18 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   }
   over += swap_rows16(over);
   over += swap_halves(over);
-  if (g == 0 && live && !(apart >> lq & 1)) delta.p[bh * Lq + q] = dl + over;
+  // rows that are out of the sums, and those that are not finite, which may be so by an infinity or NaN times the weight 0 of a key that they do not see
+  float none = over * 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) none = __builtin_fmaf(dq[db][i], 0.f, none);
+  const uint32_t alone = apart | rows_of_lanes(__ballot(live && !(none == 0.f)));
+  if (g == 0 && live && !(alone >> lq & 1)) delta.p[bh * Lq + q] = dl + over;
   if (lane == 0) delta.apart[(bh * nq + qb) * kWaves + wave] = apart;
   const int row = q0 + (lq & 12) + g;
-  if (__builtin_expect(apart != 0, 0)) {  // rows that are out of the sums
-    for (uint32_t left = apart; left; left &= left - 1) {
+  if (__builtin_expect(alone != 0, 0)) {
+    for (uint32_t left = alone; left; left &= left - 1) {
       const int r = q0 + __builtin_ctz(left), see = !bias.causal || origin + r + 1 > n ? n : origin + r + 1;
       const uint16_t* const dp = dO.p + (long)b * dO.batch + r * dO.row + (long)head * DH;
       ApartRow<DH> x{Q.p + (long)b * Q.batch + r * Q.row + (long)head * DH, k_base, K.row, s_bias, -(origin + r), far, scale, {0.f, 0.f}};
@@ -238,8 +241,9 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
         d = __builtin_fmaf(w, x.product(dp, v_base + (long)j * V.row), d);
       }
       l = wave_sum(l);
-      d = wave_sum(d) / l;
-      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j)) / l * (x.product(dp, v_base + (long)j * V.row) - d); }, k_base, K.row, 0, see,
+      const float by = l == 0.f ? 0.f : 1.0f / l;
+      d = wave_sum(d) * by;
+      ApartRow<DH>::weighted([&](int j) { return __builtin_amdgcn_exp2f(x.logit(j)) * by * (x.product(dp, v_base + (long)j * V.row) - d); }, k_base, K.row, 0, see,
                              lane, sum);
 #pragma unroll
       for (int e = 0; e < DH / 64; ++e) dQ.p[(long)b * dQ.batch + r * dQ.row + (long)head * DH + lane + 64 * e] = f32_to_bf16(sum[e] * bias.scale);
@@ -247,7 +251,7 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
     }
   }
   put_columns<DB>(dq, bias.scale, dQ.p + (long)b * dQ.batch + row * dQ.row + (long)head * DH + 8 * (lq & 3),
-                  row < (int)Lq && !(apart >> ((lq & 12) + g) & 1), lane);
+                  row < (int)Lq && !(alone >> ((lq & 12) + g) & 1), lane);
 #endif
 }
 
@@ -290,7 +294,8 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
 
   const Place place = place_of(blockIdx.x, gridDim.x, B, H / group, nk, 1);
   const int b = place.b, kv_head = place.head, kt = place.tile;
-  const int n = __builtin_amdgcn_readfirstlane(bias.keys(b, Lk)), origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int origin = __builtin_amdgcn_readfirstlane(bias.origin(b));
+  const int n = __builtin_amdgcn_readfirstlane(bias.seen(b, Lk, origin + (int)Lq - 1));  // keys that some query sees
   const int k0 = kt * kTileQueries + wave * 16 * NB;  // the wave's first key
   const int tiles = (int)((Lq + kTileKeys - 1) / kTileKeys);
   int first_tile = 0;
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
     first_tile = q <= 0 ? 0 : q / kTileKeys < tiles ? q / kTileKeys : tiles;
   }
   const int each = kt * kTileQueries < n ? tiles - first_tile : 0;
-  // a column behind the last key holds that key again, with a bias of -inf
+  // a column behind the last key has zeros for it, with a bias of -inf
   bool counts[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) counts[nb] = k0 + 16 * nb + lq < n;
@@ -351,7 +356,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) asm volatile("" : "+v"(kf[nb][kc]), "+v"(vf[nb][kc]));  // resident before the loop, which would wait for them at every tile otherwise
+    for (int kc = 0; kc < KC; ++kc) {
+      if (!counts[nb]) kf[nb][kc] = vf[nb][kc] = bf16x8{};
+      asm volatile("" : "+v"(kf[nb][kc]), "+v"(vf[nb][kc]));  // resident before the loop, which would wait for them at every tile otherwise
+    }
   for (int i = lane; i < 16 * ROW; i += 64) s_skew[i] = 0.f;
   if (tid < kNone) s_none[-tid] = -INFINITY;
 
@@ -452,7 +460,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (nearest + 16 * (nb - qb) + lq - 4 * g - e > 0) s[qb][nb][e] = -INFINITY;
+                if (nearest + 16 * (nb - qb) + lq - 4 * g - e > 0) {
+                  s[qb][nb][e] = -INFINITY;
+                  dp[qb][nb][e] = 0.f;  // an infinity or NaN of the key is not the query's
+                }
         }
         bf16x8 pf[NB], ds[NB];
 #pragma unroll
