@@ -278,6 +278,7 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),
  *   dtable dev fp32 [n_buckets, H]. A query behind its sequence's length is one like the others: its dO has to be zeros if it is not to count.
+ *   Infinities and NaN in Q and dO reach the gradients of keys ahead of their query too, causal, and dtable.
  *   steps: of dO, dQ, dK, dV, as above. Every sum is made in one order, so that equal calls give equal bits.
  *   ws  dev, chorus_attention_bias_backward_workspace_bytes bytes; scratch of this call alone. Outputs must not overlap inputs. B, Lq or Lk of 0:
  *   CHORUS_E_SHAPE (the forward pass accepts them).

@@ -598,6 +598,10 @@ __global__ __launch_bounds__(KeyShape<DH>::kThreads, 2) void bias_dkv_kernel(Row
   }
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
+    if (!counts[nb]) {  // zeros, and no infinity or NaN of a gradient times 0
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dk[nb][db] = dv[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     const int k = k0 + 16 * nb + (lq & 12) + g;
     const long at = (long)kv_head * DH + 8 * (lq & 3);
     put_columns<DB>(dk[nb], bias.scale, dK.p + (long)b * dK.batch + k * dK.row + at, k < (int)Lk, lane);
