@@ -245,6 +245,8 @@ int32_t chorus_attention_blocks(const uint16_t* Q, const uint16_t* K, const uint
 int32_t chorus_quant_rows_i8(const uint16_t* X, int64_t ld, int8_t* out, float* scale, int64_t M, int32_t K, int32_t Kp, void* stream);
 int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int64_t M, int32_t N, int32_t K,
                        int32_t epilogue, void* out, const float* bias, const float* gate0, const float* gate1, float scale, void* stream);
+/* Which kernels that product takes, as chorus_gemm_bf16_plan tells it (kernel 0: that of few rows; one slice). Host only; M from 1. */
+int32_t chorus_gemm_i8_plan(int64_t M, int32_t N, int32_t K, int32_t epilogue, chorus_gemm_plan* out);
 
 /* ------------------------------------------------------------------------
  * Attention with a learned bias by the distance between query and key, as text encoders (and decoders) have it, over a padded batch, and its
@@ -327,6 +329,9 @@ int32_t chorus_attention_bias_backward(const chorus_bias_attention* a, const cho
 #define CHORUS_ACT_GELU 0
 #define CHORUS_ACT_SILU 1
 int32_t chorus_gated_ffn(const uint16_t* X, const uint16_t* W, int32_t act, uint16_t* H, uint16_t* pre, int64_t M, int32_t F, int32_t K, void* stream);
+/* Which kernels that takes, as chorus_gemm_bf16_plan tells it for a product of 2 F columns (kernel 0: that of few rows, 6: 256 x 192 tiles; one slice). Host
+ * only; M from 1. */
+int32_t chorus_gated_ffn_plan(int64_t M, int32_t F, int32_t K, chorus_gemm_plan* out);
 size_t chorus_gated_ffn_backward_workspace_bytes(int64_t M, int32_t F, int32_t K);
 int32_t chorus_gated_ffn_backward(const uint16_t* X, const uint16_t* W, const uint16_t* pre, const uint16_t* dH, int32_t act, uint16_t* dX, void* dW,
                                   int32_t dw_epilogue, int64_t M, int32_t F, int32_t K, void* ws, size_t ws_bytes, void* stream);

@@ -185,12 +185,14 @@ def _bind_ops(lib):
         "chorus_attention_blocks": (i32, [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, i32, vp, sz, vp]),
         "chorus_quant_rows_i8": (i32, [vp, i64, vp, vp, i64, i32, i32, vp]),
         "chorus_gemm_i8": (i32, [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp, f32, vp]),
+        "chorus_gemm_i8_plan": (i32, [i64, i32, i32, i32, C.POINTER(GemmPlan)]),
         "chorus_bias_buckets": (i32, [i32, i32, i32, C.POINTER(i32)]),
         "chorus_attention_bias_workspace_bytes": (sz, [C.POINTER(BiasAttention)]),
         "chorus_attention_bias": (i32, [C.POINTER(BiasAttention)] + [vp] * 11 + [sz, vp]),
         "chorus_attention_bias_backward_workspace_bytes": (sz, [C.POINTER(BiasAttention)]),
         "chorus_attention_bias_backward": (i32, [C.POINTER(BiasAttention), C.POINTER(BiasAttentionSteps)] + [vp] * 16 + [sz, vp]),
         "chorus_gated_ffn": (i32, [vp, vp, i32, vp, vp, i64, i32, i32, vp]),
+        "chorus_gated_ffn_plan": (i32, [i64, i32, i32, C.POINTER(GemmPlan)]),
         "chorus_gated_ffn_backward_workspace_bytes": (sz, [i64, i32, i32]),
         "chorus_gated_ffn_backward": (i32, [vp, vp, vp, vp, i32, vp, vp, i32, i64, i32, i32, vp, sz, vp]),
         "chorus_glue_workspace_bytes": (sz, [i32, i32, i64]),
@@ -695,6 +697,13 @@ def chorus_gemm_i8(A, a_scale, W, w_scale, epilogue, out, bias=None, gate0=None,
     return out
 
 
+def chorus_gemm_i8_plan(M, N, K, epilogue):
+    """(rows of the first launch on kernel 3, kernel of the others, 0: few rows) of chorus_gemm_i8; host only."""
+    out = GemmPlan()
+    _status("chorus_gemm_i8_plan", load().chorus_gemm_i8_plan(M, N, K, epilogue, C.byref(out)))
+    return out.head_rows, out.kernel
+
+
 def chorus_bias_buckets(n_buckets, far, both_sides=True, device="cuda"):
     """int32 [2 far + 1]: the usual buckets of the distances -far .. far of a key from its query, on `device`."""
     out = (C.c_int32 * (2 * max(int(far), 0) + 1))()
@@ -798,6 +807,13 @@ def chorus_gated_ffn(X, W, act, H, pre=None):
     _chk_words(pre, "pre", (M, 2 * F))
     _status("chorus_gated_ffn", lib.chorus_gated_ffn(_p(X), _p(W), int(act), _p(H), _p(pre), M, F, K, _stream()))
     return H
+
+
+def chorus_gated_ffn_plan(M, F, K):
+    """(rows of the first launch on kernel 3, kernel of the others, 0: few rows, 6: 256 x 192 tiles) of chorus_gated_ffn; host only."""
+    out = GemmPlan()
+    _status("chorus_gated_ffn_plan", load().chorus_gated_ffn_plan(M, F, K, C.byref(out)))
+    return out.head_rows, out.kernel
 
 
 def chorus_gated_ffn_backward_workspace_bytes(M, F, K) -> int:

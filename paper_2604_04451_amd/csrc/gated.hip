@@ -141,6 +141,15 @@ int32_t launch_gated_tile(int tile, const Call& c, long M, int F, int K, hipStre
   }
 }
 
+// One round of 256 x 256 tiles that leaves units without one is a round of 256 x 192 tiles where all of those have a unit (F = 10240, K = 4096, 512
+// rows: 160 tiles 78 us, 214 of these 67; 2048 x 2560 x 4096 79 and 67, x 1024 27 and 23). In all other products of 80 (M 100 to 3000, F 1024 to 13824) the
+// choice by the estimates was the faster or as fast.
+TileCut gated_tiles(int64_t M, int32_t F, int32_t K) {
+  TileCut cut = gemm_tiles(M, 2 * F, K, CHORUS_EPI_GELU_BF16);
+  if (cut.head_rows == 0 && cut.tile == kTile256 && (M + 255) / 256 * ((F + 95) / 96) <= 256) cut.tile = kTile192;
+  return cut;
+}
+
 // few rows: the wave that joins a strip's sums
 template <int ACT>
 struct StripGated {
@@ -309,14 +318,21 @@ int32_t chorus_gated_ffn(const uint16_t* X, const uint16_t* W, int32_t act, uint
     if (act == CHORUS_ACT_GELU) return launch_skinny<MmaBf16, 2>(X, W, W2, (int)M, F, K, StripGated<CHORUS_ACT_GELU>{H, pre, F}, s);
     return launch_skinny<MmaBf16, 2>(X, W, W2, (int)M, F, K, StripGated<CHORUS_ACT_SILU>{H, pre, F}, s);
   }
-  TileCut cut = gemm_tiles(M, 2 * F, K, CHORUS_EPI_GELU_BF16);
-  // One round of 256 x 256 tiles that leaves units without one is a round of 256 x 192 tiles where all of those have a unit (F = 10240, K = 4096, 512
-  // rows: 160 tiles 78 us, 214 of these 67; 2048 x 2560 x 4096 79 and 67, x 1024 27 and 23). In all other products of 80 (M 100 to 3000, F 1024 to 13824) the
-  // choice by the estimates was the faster or as fast.
-  if (cut.head_rows == 0 && cut.tile == kTile256 && (M + 255) / 256 * ((F + 95) / 96) <= 256) cut.tile = kTile192;
+  const TileCut cut = gated_tiles(M, F, K);
   if (cut.head_rows) CHK_STATUS(launch_gated_tile(kTile256, Call{X, W, H, pre, act}, cut.head_rows, F, K, s));
   const size_t head = (size_t)cut.head_rows;
   return launch_gated_tile(cut.tile, Call{X + head * K, W, H + head * F, pre ? pre + head * 2 * F : nullptr, act}, (long)M - cut.head_rows, F, K, s);
+}
+
+int32_t chorus_gated_ffn_plan(int64_t M, int32_t F, int32_t K, chorus_gemm_plan* out) {
+  CHK_STATUS(check_gated(M, F, K, CHORUS_ACT_GELU));
+  if (!out || M == 0) return CHORUS_E_ARG;
+  *out = chorus_gemm_plan{0, 0, 1};
+  if (skinny_rows(M, 2L * F)) return CHORUS_OK;
+  const TileCut cut = gated_tiles(M, F, K);
+  out->head_rows = cut.head_rows;
+  out->kernel = cut.tile == kTile192 ? 6 : kTileNumber[cut.tile];
+  return CHORUS_OK;
 }
 
 size_t chorus_gated_ffn_backward_workspace_bytes(int64_t M, int32_t F, int32_t K) {

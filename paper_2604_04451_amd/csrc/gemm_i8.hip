@@ -246,6 +246,12 @@ struct StripI8 {
   }
 };
 
+int32_t check_i8(int64_t M, int32_t N, int32_t K, int32_t epilogue) {
+  if (M < 0 || N <= 0 || K <= 0 || epilogue < CHORUS_EPI_BF16 || epilogue > CHORUS_EPI_RESID) return CHORUS_E_ARG;
+  if (K % kStep || N % 8 || K > kMostK || N > kMostN) return CHORUS_E_SHAPE;
+  return CHORUS_OK;
+}
+
 int32_t launch_i8_few(const Operands& x, long M, int N, int K, int epi, const EpiArgs& ep, hipStream_t s) {
 #define FEW(E) return launch_skinny<MmaI8, 1>(x.A, x.W, nullptr, (int)M, N, K, StripI8<E>{x.a_scale, x.w_scale, ep, N}, s)
   switch (epi) {
@@ -281,8 +287,7 @@ int32_t chorus_quant_rows_i8(const uint16_t* X, int64_t ld, int8_t* out, float* 
 
 int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, int64_t M, int32_t N, int32_t K,
                        int32_t epilogue, void* out, const float* bias, const float* gate0, const float* gate1, float scale, void* stream) {
-  if (M < 0 || N <= 0 || K <= 0 || epilogue < CHORUS_EPI_BF16 || epilogue > CHORUS_EPI_RESID) return CHORUS_E_ARG;
-  if (K % kStep || N % 8 || K > kMostK || N > kMostN) return CHORUS_E_SHAPE;
+  CHK_STATUS(check_i8(M, N, K, epilogue));
   if (M == 0) return CHORUS_OK;
   if (!A || !a_scale || !W || !w_scale || !out) return CHORUS_E_ARG;
   if (!aligned16(A) || !aligned16(a_scale) || !aligned16(W) || !aligned16(w_scale) || !aligned16(out) || !aligned16(bias) || !aligned16(gate0) ||
@@ -300,6 +305,17 @@ int32_t chorus_gemm_i8(const int8_t* A, const float* a_scale, const int8_t* W, c
   rest.out = static_cast<uint8_t*>(out) + (size_t)cut.head_rows * (size_t)N * elt;
   const Operands tail{x.A + (size_t)cut.head_rows * (size_t)units, x.W, a_scale + cut.head_rows, w_scale};
   return launch_i8_tile(cut.tile, tail, (long)M - cut.head_rows, N, units, epilogue, rest, s);
+}
+
+int32_t chorus_gemm_i8_plan(int64_t M, int32_t N, int32_t K, int32_t epilogue, chorus_gemm_plan* out) {
+  CHK_STATUS(check_i8(M, N, K, epilogue));
+  if (!out || M == 0) return CHORUS_E_ARG;
+  *out = chorus_gemm_plan{0, 0, 1};
+  if (skinny_rows(M, N)) return CHORUS_OK;
+  const TileCut cut = gemm_tiles(M, N, K / 2, epilogue);
+  out->head_rows = cut.head_rows;
+  out->kernel = kTileNumber[cut.tile];
+  return CHORUS_OK;
 }
 
 }  // extern "C"
