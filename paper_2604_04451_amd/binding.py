@@ -757,6 +757,7 @@ def chorus_attention_bias(Q, K, V, O, table, bucket, lens=None, first=None, caus
     other half of the result's bits) for the backward pass."""
     lib = load()
     a = _bias_attention(Q, K, V, O, table, bucket, lens, first, causal, scale, lse, rest)
+    _chk(ws, torch.uint8, "ws")
     if ws is None:
         need = lib.chorus_attention_bias_workspace_bytes(C.byref(a))
         ws = _ws(need, Q.device) if need else None
@@ -777,6 +778,7 @@ def chorus_attention_bias_backward(Q, K, V, O, rest, lse, dO, table, bucket, dQ,
     q, k = Q.shape, K.shape
     steps = BiasAttentionSteps(*_heads(dO, "dO", q), *_heads(dQ, "dQ", q), *_heads(dK, "dK", k), *_heads(dV, "dV", k))
     _chk(dtable, torch.float32, "dtable", (a.n_buckets, a.H))
+    _chk(ws, torch.uint8, "ws")
     if ws is None:
         ws = _ws(lib.chorus_attention_bias_backward_workspace_bytes(C.byref(a)), Q.device)
     _status("chorus_attention_bias_backward",
@@ -833,6 +835,7 @@ def chorus_gated_ffn_backward(X, W, pre, dH, act, dX, dW, accumulate=False, ws=N
     _chk(dX, torch.bfloat16, "dX", (M, K))
     full = accumulate or (dW is not None and dW.dtype == torch.float32)
     _chk(dW, torch.float32 if full else torch.bfloat16, "dW", (2 * F, K))
+    _chk(ws, torch.uint8, "ws")
     if ws is None:
         ws = _ws(lib.chorus_gated_ffn_backward_workspace_bytes(M, F, K), X.device)
     _status("chorus_gated_ffn_backward",
