@@ -255,7 +255,7 @@ int32_t chorus_gemm_i8_plan(int64_t M, int32_t N, int32_t K, int32_t epilogue, c
  *   logit(i, j) = scale * q_i . k_j + table[bucket[clamp(d, -far, far) + far]][head],  d = j - (first[b] + i)
  *   query i of sequence b sees the keys j < lens[b] (at most Lk), and with causal only those with d <= 0
  *   O = softmax(logits) V; a row that sees no key, or only logits of -inf, is zeros. Keys and values behind lens[b] are not read.
- *   What a query does not see has no part in its row, infinities and NaN included; rows that are not finite are made one by one, which is slow.
+ *   What a query does not see has no part in its row, infinities and NaN included; rows that are not finite though their logits are, are made one by one, which is slow.
  *
  * chorus_bias_attention
  *   B, Lq, Lk, H, Hk, dh   sequences, queries and keys of each, heads, heads of keys and values (H % Hk == 0; head h reads h / (H / Hk)); dh in {64, 128}

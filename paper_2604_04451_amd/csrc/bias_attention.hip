@@ -302,14 +302,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
     }
     const float l = SPLIT ? l_run[rb] : l_sum[rb][0], inv = l == 0.f ? 0.f : 1.0f / l;  // no key at all: a row of zeros
     const int row = row0 + 16 * rb, mine = q0 + 16 * rb + out_q, count = (int)Lq;
-    // rows that are out of the sums: all their logits are far below the reference, or it is too large. And rows that are not finite, which may be so by
-    // an infinity or NaN times the weight 0 of a key that they do not see, or the other part of a weight.
+    // rows that are out of the sums: all their logits are far below the reference, or it is too large. And rows that are not finite though their weights are,
+    // which may be so by an infinity or NaN times the weight 0 of a key that they do not see, or the other part of a weight.
     float none = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int i = 0; i < 4; ++i) none = __builtin_fmaf(o[db][rb][i], 0.f, none);
-    const uint32_t apart = rows_of_lanes(__ballot(mine < count && (!(none == 0.f) || (seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))))));
+    const uint32_t apart = rows_of_lanes(__ballot(mine < count && ((!(none == 0.f) && l * 0.f == 0.f) || (seen[rb] && (l < kLeastSum || out_of_sums(m_run[rb]))))));
     all_apart |= apart << 16 * rb;
     const bool live = row < count && !(apart >> ((out_q & 12) + out_g) & 1), mine_live = mine < count && !(apart >> out_q & 1);
     if (slices > 1) {
@@ -561,13 +561,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void bias_few_kernel(Rows Q, Row
 #pragma unroll
   for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(s_o + (wave * kFewRows + lq) * (DH + 4) + 16 * db + 4 * g) = o[db];
   if (g == 0) s_share[wave * kFewRows + lq] = Share{ref, l_run};
-  // Rows that are not finite are made again of the keys that they see, as in the tiled kernel: this wave's part of them, with its weights.
+  // Rows that are not finite though their weights are: made again of the keys that they see, as in the tiled kernel: this wave's part of them, with its weights.
   float none = 0.f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 4; ++i) none = __builtin_fmaf(o[db][i], 0.f, none);
-  for (uint32_t left = rows_of_lanes(__ballot(lq < live_rows && !(none == 0.f))); __builtin_expect(left != 0, 0); left &= left - 1) {
+  for (uint32_t left = rows_of_lanes(__ballot(lq < live_rows && !(none == 0.f) && l_run * 0.f == 0.f)); __builtin_expect(left != 0, 0); left &= left - 1) {
     const int r = __builtin_ctz(left), of = r / Lq, qi = r - of * Lq, see = !bias.causal || origin + qi + 1 > n ? n : origin + qi + 1;
     const Reference at{__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ref.hi), r)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ref.lo), r))};
     const ApartRow<DH> x{Q.p + (long)b * Q.batch + (long)qi * Q.row + (long)(head0 + of) * DH, k_base, K.row, s_bias + of * width, -(origin + qi), far, scale, at};

@@ -217,13 +217,14 @@ __global__ __launch_bounds__(64 * kWaves, DH == 64 ? 4 : 2) void bias_dq_kernel(
   }
   over += swap_rows16(over);
   over += swap_halves(over);
-  // rows that are out of the sums, and those that are not finite, which may be so by an infinity or NaN times the weight 0 of a key that they do not see
+  // rows that are out of the sums, and those that are not finite though their result is, which may be so by an infinity or NaN times the weight 0 of a key
+  // that they do not see
   float none = over * 0.f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 4; ++i) none = __builtin_fmaf(dq[db][i], 0.f, none);
-  const uint32_t alone = apart | rows_of_lanes(__ballot(live && !(none == 0.f)));
+  const uint32_t alone = apart | rows_of_lanes(__ballot(live && !(none == 0.f) && dl * 0.f == 0.f));
   if (g == 0 && live && !(alone >> lq & 1)) delta.p[bh * Lq + q] = dl + over;
   if (lane == 0) delta.apart[(bh * nq + qb) * kWaves + wave] = apart;
   const int row = q0 + (lq & 12) + g;
