@@ -269,13 +269,15 @@ int32_t chorus_gemm_i8_plan(int64_t M, int32_t N, int32_t K, int32_t epilogue, c
  * chorus_attention_bias
  *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
  *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
- *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass; without rest, of the weights
- *               as they are rounded to bf16
+ *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass; without rest and of more
+ *               than 16 queries, of the weights as they are rounded to bf16
  *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
  *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe, with rest to 16 bits.
  *   Biases of any size: keys behind a finite mask, the lowest value of the type included, weigh nothing beside others and alike by themselves
- *   (products count beside a largest logit of up to 2^60). Rows whose logits are all below -80 or beyond 700 are made one by one, which is slow.
+ *   (products count beside a largest bias of up to 2^60). Rows whose logits are all below -80 or beyond 700 are made one by one, but for calls of up to 16
+ *   queries without rest. That is slow: 512 and 256 tokens of 64 heads, all rows so, 2.4 ms instead of 17 us; 8191 tokens, 12 heads of 128, with
+ *   gradients 0.43 s instead of 2.1 ms.
  *   Outputs must not overlap inputs.
  * chorus_attention_bias_backward: from dO, and O, rest and lse of the forward pass,
  *   dQ dev bf16 [.., H heads], dK, dV dev bf16 [.., Hk heads] (summed over the heads that share them; rows from lens[b] to Lk are zeros),

@@ -9,9 +9,9 @@
 // The bias of a distance is in LDS, in powers of two, `far` and a tile's width to either side. A wave's 64 x 32 logits read it only where some
 // distance is below `far`; tiles beyond have one value. The sums of the matrix pipe start at minus the row's reference, so that a logit
 // becomes the exponent of its weight in one fma.
-// Measured: two prompts of 512 and 256 tokens, 64 heads of 64, 17.5 us; of that 7.5 before the first and behind the last step, for which the lengths, the biases
+// Measured: two prompts of 512 and 256 tokens, 64 heads of 64, 17 to 18 us; of that 7.5 before the first and behind the last step, for which the lengths, the biases
 // and the first tiles are fetched one behind the other; a step 1.1 us, bound by the vector pipe's 160 instructions and 32 exponentials for 32
-// MFMAs. Halving the rows of a workgroup changed nothing. 8191 tokens, 12 heads of 128, weights in two parts: 605 us, 910 TFLOP/s with the second parts' products.
+// MFMAs. Halving the rows of a workgroup changed nothing. 8191 tokens, 12 heads of 128, weights in two parts: 612 us, 1010 TFLOP/s with the second parts' products.
 #include "bias_attention.h"
 
 namespace chorus {
@@ -37,9 +37,9 @@ struct Outputs {
   float* lse;      // [B, H, Lq]
 };
 
-// SPLIT: for the backward pass a weight goes to the matrix pipe in two parts of 8 bits, and the other half of the result's bits goes out as well: delta =
-// dO . O then has 16 bits (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of
-// 8 bits; 8191 tokens, 12 heads of 128 500 to 605 us).
+// SPLIT: for the backward pass a weight goes to the matrix pipe in two parts of 8 bits, 16 together, and the other half of the result's bits goes out as well:
+// delta = dO . O then has 16 bits in the products for dQ (relative error of dQ against 64 bits 0.0024, 0.0025 with weights of 8 bits; 8191 tokens, 12 heads of
+// 128 486 to 612 us). The second pass and the table's sums have their delta from the first one's sums, whatever that of dO . O was.
 template <int DH, bool SPLIT>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(Rows Q, Rows K, Rows V, Outputs out, BiasArgs bias, float* __restrict__ part, long Lq,
                                                                 long Lk, int B, int H, int group, int nq, int slices) {
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void bias_attention_kernel(R
 // Few queries: what they take is the time to read the keys and values. Up to 16 rows, the queries of as many of the heads that share keys as fit, make
 // one block of columns for the matrix pipe; the eight waves of a workgroup take every eighth tile of 64 keys each, by themselves: keys straight into
 // the registers that the matrix pipe reads, values through a region of LDS of the wave's own for their columns, both requested a tile ahead. No barrier
-// but for the join of the waves at the end. Four sequences of 64 heads of 64, one query each over 1025 to 4097 keys: 33 us, 5 TB/s; 45 where no cache holds a part
+// but for the join of the waves at the end. Four sequences of 64 heads of 64, one query each over 1025 to 4097 keys: 35 us, 4.8 TB/s; 48 where no cache holds a part
 // of them, for the longest sequence's workgroups. Two slices of each were 4 % faster there and 1 % slower here, four 25 % slower here.
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 16, kFewWaves = 8;

@@ -54,8 +54,8 @@ __device__ __forceinline__ float kept16(uint32_t w) {  // the low half
 // Forward: gemm16_loop with tiles whose columns are 16 of the gate and 16 of the other factor in turn, so that a lane's even blocks hold
 // the gate at the very places where its odd ones hold the factor, and their product needs no exchange. x is read once for both. SAVE: the two
 // projections go out as well, in 16 bits, for the backward pass.
-// Bound as the product of as many columns is: 512 x 10240 x 4096 74 us, 1170 TFLOP/s; 4096 x 10240 x 4096 with SAVE 555 us, 1240 TFLOP/s, of which the three
-// outputs' 250 MB are 50.
+// Bound as the product of as many columns is: 512 x 10240 x 4096 68 us with the weights in the last-level cache, 1260 TFLOP/s, 80 without; 4096 x 10240 x 4096
+// with SAVE 560 us, 1230 TFLOP/s, of which the three outputs' 250 MB are 50.
 // ---------------------------------------------------------------------------
 template <int ACT, bool SAVE, int WBM, int WBN, int C>
 __global__ __launch_bounds__(256, 1) void gated_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, uint16_t* __restrict__ H,
@@ -142,7 +142,7 @@ int32_t launch_gated_tile(int tile, const Call& c, long M, int F, int K, hipStre
 }
 
 // One round of 256 x 256 tiles that leaves units without one is a round of 256 x 192 tiles where all of those have a unit (F = 10240, K = 4096, 512
-// rows: 160 tiles 78 us, 214 of these 67; 2048 x 2560 x 4096 79 and 67, x 1024 27 and 23). In all other products of 80 (M 100 to 3000, F 1024 to 13824) the
+// rows, weights in the last-level cache: 160 tiles 75 us, 214 of these 68; not there: 85 and 80; 2048 x 2560 x 4096 75 and 67, x 1024 25 and 22). In all other products of 80 (M 100 to 3000, F 1024 to 13824) the
 // choice by the estimates was the faster or as fast.
 TileCut gated_tiles(int64_t M, int32_t F, int32_t K) {
   TileCut cut = gemm_tiles(M, 2 * F, K, CHORUS_EPI_GELU_BF16);

@@ -17,8 +17,9 @@ constexpr float kTiny = 0x1p-100f, kHuge = 0x1p100f;
 
 // ---------------------------------------------------------------------------
 // Rows to codes: T threads a row, which stays in their registers between the search of its largest value and the rounding (V pieces
-// of 8 values a thread; longer rows are read twice). One read, half as much written; memory bound: 32760 x 1536 37 us, 13103 x 8960 84, 4.1 and 4.2 TB/s with
-// the codes; one row 4 us. The tokens are read past the caches, which have the codes for the product then (both calls, 13103 x 8960: 224 us, so 219).
+// of 8 values a thread; longer rows are read twice). One read, half as much written; memory bound: 32760 x 1536 34 us, 13103 x 8960 67, 4.4 and 5.3 TB/s with
+// the codes, in a row of calls (in a trace of few of them 38 and 86); one row 4 us. The tokens are read past the caches, which have the codes for the product
+// then: 67 and, for the product to fp32, 160 us each in a row of its own, 213 to 222 by card both in turn, 224 with tokens read as usual.
 // The code is the whole number nearest to 127 x / max, halves to even, as if that quotient were exact. fp32 brings q = x (127 / max)
 // to within 1.5 units in the last place, so that round(q) is off by one at most, near a half. What is left, 127 x - q max, is exact in an
 // fma: 127 x and q max have 15 bits each, and for q != 0 their units are at most 2^9 apart. It is compared with max / 2.
@@ -106,9 +107,9 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const uint16_t* __restr
 // ---------------------------------------------------------------------------
 // The product: gemm16_loop with 8-bit operands, which takes 128 values in the bytes of 64. The scales go into the sums before the
 // epilogue of the bf16 product, which adds the bias, takes the GELU or adds to the residual.
-// Bound by the delivery of the operands, and by the epilogue where K is short, which nothing of the loop runs beside: 32760 x 8960 x 1536 with GELU 490
-// to 580 us by card, 1840 to 1560 TOP/s (the loop alone 2870 TOP/s, GELU and its conversions 63 us, all of the epilogue 170); 13103 x 1536 x 8960 to fp32
-// 187 us, 1930 TOP/s. Other tiles for either, and for 512 x 1536 x 4096 (11 us), were no faster.
+// Bound by the delivery of the operands, and by the epilogue where K is short, which nothing of the loop runs beside: 32760 x 8960 x 1536 with GELU 495 us,
+// 1820 TOP/s (the loop alone 2870 TOP/s, GELU and its conversions 63 us, all of the epilogue 170), in bf16 774; 13103 x 1536 x 8960 to fp32 157 to 160 us, 2270
+// TOP/s, with the gated residual 166, in bf16 302 and 304; 32760 x 1536 x 8960 with the gated residual 364, in bf16 670. Other tiles for either, and for 512 x 1536 x 4096 (11 us), were no faster.
 // ---------------------------------------------------------------------------
 template <int EPI, int WBM, int WBN, int C>
 __global__ __launch_bounds__(256, 1) void gemm_i8_kernel(const uint16_t* __restrict__ A, const uint16_t* __restrict__ W, long M, int N, int K,
