@@ -270,7 +270,8 @@ int32_t chorus_gemm_i8_plan(int64_t M, int32_t N, int32_t K, int32_t epilogue, c
  *   Q, K, V, O  dev bf16;  table dev fp32 [n_buckets, H];  bucket dev int32 [2 far + 1] (an entry outside the table: no bias)
  *   lens        dev int32 [B], the keys of each sequence, or NULL (Lk each);  first dev int32 [B], the position of query 0 among the keys, or NULL (0)
  *   lse         dev fp32 [B, H, Lq] or NULL: the logarithm of the sum of exp(logits) (-inf: no key), for the backward pass; without rest and of more
- *               than 16 queries, of the weights as they are rounded to bf16
+ *               than 16 queries, of the weights as they are rounded to bf16. Biases beyond +-2^90 powers of two, the lowest value of the type among
+ *               them, count as those, and so end there
  *   rest        dev 16-bit words laid out as O, or NULL: the half of the fp32 result's bits that O's rounding leaves off, for the backward pass
  *   ws          dev, chorus_attention_bias_workspace_bytes bytes (0: none, ws may be NULL); scratch of this call alone
  *   Logits, weights' sums and results are fp32; the weights are rounded to bf16 for the matrix pipe, with rest to 16 bits.

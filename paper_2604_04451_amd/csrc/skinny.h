@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
           p.a[u][h][mb] = bf16x8{};
-          if (live[mb] && g + u < groups) p.a[u][h][mb] = *reinterpret_cast<const bf16x8*>(a[mb] + at);
+          if (live[mb]) p.a[u][h][mb] = *reinterpret_cast<const bf16x8*>(a[mb] + at);
         }
       }
   };
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(const uint16_
   for (; g < groups; g += step) {
     if (g + step < groups) load(next, g + step);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U && g + u < groups; ++u)  // what is behind the last group is that one again
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
